@@ -254,6 +254,91 @@ sh_status switchhead_get_intermediates(const sh_shape* shape,
                                        float* Q, float* K, float* V, float* ctx, float* lse,
                                        void* hip_stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Operators beside the layer: attention over packed sequences with grouped heads, attention of sequences that share a
+ * prefix, and the norms of queries and keys with the rotation.  The conventions above hold for them too.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/*
+ * Attention over packed sequences.  Tensors hold the rows (tokens) of all sequences one behind the other:
+ *   Q, O (dO, dQ)  [total_q, nheads, d_head]       K, V (dK, dV)  [total_k, nkv_heads, d_head]
+ * in storage type `dtype`, each with the strides below (elements; 0 = dense in that order).  A gradient lies as its tensor
+ * does: dQ has Q's strides, dK K's, dV V's, dO O's.  Query head h reads kv head h / (nheads / nkv_heads).
+ *
+ * Sequence i owns the query rows q_offsets[i] .. q_offsets[i + 1] - 1 and the key rows k_offsets[i] .. k_offsets[i + 1] - 1; with
+ * q_lengths (k_lengths) only the first q_lengths[i] (k_lengths[i]) of them, as in a padded batch or a cache with a place of one
+ * length per sequence.  All four are int32 arrays on the device (offsets nseq + 1, lengths nseq; lengths may be NULL).  Offsets
+ * must not fall.  They are not checked on the host; whatever they hold, no row outside the tensors is touched.
+ * Rows that belong to no sequence are neither read nor written.
+ *
+ *   O_i = sum_u p_iu V_u,   p_iu = exp(scale <Q_i, K_u> - lse_i),   lse_i = log sum_u exp(scale <Q_i, K_u>)
+ *
+ * over the keys u that query i of its sequence sees: all rows of the prefix, and of its n_k own keys all, or with `causal` those
+ * with u <= (n_k - n_q) + i (the last query sees every key).  A query that sees nothing has O = 0, lse = -infinity and gives
+ * no gradient.  What lies in keys and values behind a sequence's length has no influence, NaN included.
+ */
+typedef struct {
+  int32_t nseq;
+  int32_t nheads, nkv_heads, d_head;   /* nheads a multiple of nkv_heads; d_head <= 256                              */
+  int32_t causal, dtype;
+  int32_t total_q, total_k;            /* rows of Q and of K, V                                                      */
+  int32_t max_q;                       /* no sequence has more queries: further ones are treated as not there        */
+  int32_t max_k;                       /* about the most own keys of a sequence: chooses how work is split, no more   */
+  int32_t prefix;                      /* rows of K_prefix, V_prefix [prefix, nkv_heads, d_head] that every query sees
+                                          in front of its own keys; 0: none                                          */
+  float scale;                         /* > 0, or 0 for 1 / sqrt(d_head)                                             */
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
+  int64_t kp_row, kp_head, vp_row, vp_head;   /* of K_prefix, V_prefix                                               */
+} sh_attention;
+
+/* Bytes of workspace (256-byte aligned) that a forward call of this description needs, or with `backward` a forward or a backward call;
+ * 0 if the description is invalid.  Host-only.  Nothing is kept in it between calls. */
+size_t switchhead_attention_workspace_bytes(const sh_attention* a, int32_t backward);
+
+/* lse: fp32 [nheads, total_q] (natural logarithm) or NULL.  K_prefix, V_prefix: NULL without a prefix.  One or a few queries per sequence (decoding
+ * over caches), prompts and training batches are the same call.  Results repeat bit for bit.  O may not overlap an input. */
+sh_status switchhead_attention_forward(const sh_attention* a, const void* Q, const void* K, const void* V,
+                                       const void* K_prefix, const void* V_prefix,
+                                       const int32_t* q_offsets, const int32_t* q_lengths,
+                                       const int32_t* k_offsets, const int32_t* k_lengths,
+                                       void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Gradients of <O, dO>: O and lse as forward left them (same description, prefix 0).  dK, dV sum over the query heads of their kv head.
+ * Rows of sequences are overwritten, other rows left.  Deterministic: no atomics. */
+sh_status switchhead_attention_backward(const sh_attention* a, const void* Q, const void* K, const void* V,
+                                        const void* O, const void* dO, const float* lse,
+                                        const int32_t* q_offsets, const int32_t* q_lengths,
+                                        const int32_t* k_offsets, const int32_t* k_lengths,
+                                        void* dQ, void* dK, void* dV,
+                                        void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Norms of queries and keys for each head, and their rotary positions, in one pass:
+ *   n = x w / sqrt(mean(x^2) + eps)  over the d_head elements of a row and head,  y = n with each pair (2i, 2i + 1), 2i < rope_dim,
+ *   turned by positions[token] * theta^(-2i / rope_dim)
+ * (the rotation of sh_shape::rope; rope_dim 0: none).  Q -> Y_Q [tokens, nheads, d_head], K -> Y_K [tokens, nkv_heads, d_head],
+ * strides in elements, 0 = dense; nkv_heads 0: queries only, K may be NULL.  Y may be the input itself (same strides).  w_Q, w_K: [d_head]
+ * in storage type, shared by the heads, or NULL for ones.  positions: int32 [tokens] on the device (any value), or NULL: 0, 1, 2, ...
+ */
+typedef struct {
+  int32_t tokens, nheads, nkv_heads, d_head;
+  int32_t rope_dim;                    /* even, <= d_head                                                            */
+  int32_t dtype;
+  float eps;                           /* >= 0                                                                       */
+  float theta;                         /* > 0, or 0 for 10000                                                        */
+  int64_t q_row, q_head, k_row, k_head, yq_row, yq_head, yk_row, yk_head;
+} sh_qk_norm;
+
+/* Bytes of workspace of a backward call (forward needs none); 0 if invalid. */
+size_t switchhead_qk_norm_workspace_bytes(const sh_qk_norm* a);
+sh_status switchhead_qk_norm_rope_forward(const sh_qk_norm* a, const void* Q, const void* K, const void* w_Q, const void* w_K,
+                                          const int32_t* positions, void* Y_Q, void* Y_K, void* hip_stream);
+/* Q, K: the inputs of forward.  dY_Q, dY_K have the strides of Y_Q, Y_K; dQ, dK those of Q, K (they may be the dY tensors where those are
+ * the same).  dw_Q, dw_K: fp32 [d_head] sums over tokens and heads, or NULL; they repeat bit for bit.  All are overwritten. */
+sh_status switchhead_qk_norm_rope_backward(const sh_qk_norm* a, const void* Q, const void* K, const void* w_Q, const void* w_K,
+                                           const int32_t* positions, const void* dY_Q, const void* dY_K, void* dQ, void* dK,
+                                           float* dw_Q, float* dw_K, void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Description of the last error on this thread ("" if none). Never NULL. */
 const char* switchhead_last_error(void);
 

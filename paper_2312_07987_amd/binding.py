@@ -20,12 +20,27 @@ STATIC_WORKSPACE_BYTES = 16 << 20
 EXPORTS = ("switchhead_workspace_bytes", "switchhead_workspace_parts", "switchhead_forward", "switchhead_forward_static", "switchhead_backward",
            "switchhead_get_routing", "switchhead_get_intermediates", "switchhead_last_error",
            "switchhead_set_kernel_family", "switchhead_version",
-           "switchhead_profile_enable", "switchhead_profile_read")
+           "switchhead_profile_enable", "switchhead_profile_read",
+           "switchhead_attention_workspace_bytes", "switchhead_attention_forward", "switchhead_attention_backward",
+           "switchhead_qk_norm_workspace_bytes", "switchhead_qk_norm_rope_forward", "switchhead_qk_norm_rope_backward")
 
 
 class sh_shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("B", "T", "d_model", "nheads", "d_head", "E", "k", "causal", "dtype", "qk_experts", "rope", "T_q")]
+
+
+class sh_attention(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("nseq", "nheads", "nkv_heads", "d_head", "causal", "dtype", "total_q", "total_k",
+                                               "max_q", "max_k", "prefix")] + [("scale", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "o_row", "o_head",
+                                               "kp_row", "kp_head", "vp_row", "vp_head")])
+
+
+class sh_qk_norm(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("tokens", "nheads", "nkv_heads", "d_head", "rope_dim", "dtype")] +
+                [("eps", ctypes.c_float), ("theta", ctypes.c_float)] +
+                [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "yq_row", "yq_head", "yk_row", "yk_head")])
 
 
 class SwitchHeadError(RuntimeError):
@@ -75,6 +90,19 @@ def lib():
     L.switchhead_profile_read.restype = i32
     L.switchhead_profile_read.argtypes = [ctypes.c_char_p, sz, ctypes.POINTER(ctypes.c_float),
                                           ctypes.POINTER(i32), i32]
+    att, nrm = ctypes.POINTER(sh_attention), ctypes.POINTER(sh_qk_norm)
+    L.switchhead_attention_workspace_bytes.restype = sz
+    L.switchhead_attention_workspace_bytes.argtypes = [att, i32]
+    L.switchhead_attention_forward.restype = i32
+    L.switchhead_attention_forward.argtypes = [att] + [vp] * 12 + [sz, vp]
+    L.switchhead_attention_backward.restype = i32
+    L.switchhead_attention_backward.argtypes = [att] + [vp] * 14 + [sz, vp]
+    L.switchhead_qk_norm_workspace_bytes.restype = sz
+    L.switchhead_qk_norm_workspace_bytes.argtypes = [nrm]
+    L.switchhead_qk_norm_rope_forward.restype = i32
+    L.switchhead_qk_norm_rope_forward.argtypes = [nrm] + [vp] * 7 + [vp]
+    L.switchhead_qk_norm_rope_backward.restype = i32
+    L.switchhead_qk_norm_rope_backward.argtypes = [nrm] + [vp] * 12 + [sz, vp]
     _lib = L
     return L
 
@@ -169,3 +197,102 @@ def switchhead_profile_read(max_entries=64):
     n = lib().switchhead_profile_read(buf, len(buf), ms, cnt, max_entries)
     names = buf.value.decode().split("\n")[:n]
     return {names[i]: (float(ms[i]), int(cnt[i])) for i in range(n)}
+
+
+# ---- operators beside the layer ---------------------------------------------------------------------------------------------
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _launch(fn, device, stream, *args):
+    """Calls fn(*args, stream) with `device` current: its current stream where none is given."""
+    import torch
+    if device.type != "cuda":
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "the tensors must be on a GPU")
+    if device.index is not None and device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            return _check(fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else int(stream)))
+    _check(fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else int(stream)))
+
+
+def _dtype_code(t):
+    import torch
+    codes = {torch.float32: SH_F32, torch.bfloat16: SH_BF16}
+    if t.dtype not in codes:
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "tensors are float32 or bfloat16, not %s" % t.dtype)
+    return codes[t.dtype]
+
+
+def _rows(name, t, like=None, heads=None):
+    """Row and head stride of a [rows, heads, d_head] tensor, its rows' elements next to each other."""
+    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s must be [rows, heads, d_head] with the elements of a head next to each other" % name)
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s has another type, device or head width" % name)
+    if heads is not None and t.shape[1] != heads:
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s has %d heads, not %d" % (name, t.shape[1], heads))
+    rows, head = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], t.stride(1) if t.shape[1] > 1 else t.shape[2]
+    if rows == 0 or head == 0:
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s is broadcast along its rows or heads" % name)
+    return rows, head
+
+
+def make_attention(Q, K, V, O, nseq, max_q, max_k, causal=1, K_prefix=None, V_prefix=None, scale=0.0):
+    """The description of attention over these tensors: Q, O [total_q, nheads, d_head], K, V [total_k, nkv_heads, d_head], strided as they
+    are (views of a fused projection, slices of a cache).  Valid for any tensors of the same shapes and strides."""
+    q, k, v, o = _rows("Q", Q), _rows("K", K, Q), _rows("V", V, Q, K.shape[1]), _rows("O", O, Q, Q.shape[1])
+    if V.shape[0] != K.shape[0] or O.shape[0] != Q.shape[0]:
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "K and V, and Q and O, must have the same number of rows")
+    if (K_prefix is None) != (V_prefix is None):
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "K_prefix and V_prefix come together")
+    prefix, kp, vp = 0, (0, 0), (0, 0)
+    if K_prefix is not None:
+        kp, vp, prefix = _rows("K_prefix", K_prefix, Q, K.shape[1]), _rows("V_prefix", V_prefix, Q, K.shape[1]), K_prefix.shape[0]
+        if V_prefix.shape[0] != prefix:
+            raise SwitchHeadError(SH_ERR_INVALID_ARG, "K_prefix and V_prefix must have the same number of rows")
+    return sh_attention(nseq, Q.shape[1], K.shape[1], Q.shape[2], int(causal), _dtype_code(Q), Q.shape[0], K.shape[0], max_q, max_k, prefix,
+                        scale, *q, *k, *v, *o, *kp, *vp)
+
+
+def switchhead_attention_workspace_bytes(attention, backward=False):
+    return int(lib().switchhead_attention_workspace_bytes(attention, int(backward)))
+
+
+def switchhead_attention_forward(attention, Q, K, V, q_offsets, k_offsets, O, lse, workspace, q_lengths=None, k_lengths=None,
+                                 K_prefix=None, V_prefix=None, stream=None):
+    _launch(lib().switchhead_attention_forward, Q.device, stream, attention, _addr(Q), _addr(K), _addr(V), _addr(K_prefix), _addr(V_prefix),
+            _addr(q_offsets), _addr(q_lengths), _addr(k_offsets), _addr(k_lengths), _addr(O), _addr(lse),
+            _addr(workspace), workspace.numel() * workspace.element_size())
+
+
+def switchhead_attention_backward(attention, Q, K, V, O, dO, lse, q_offsets, k_offsets, dQ, dK, dV, workspace, q_lengths=None,
+                                  k_lengths=None, stream=None):
+    _launch(lib().switchhead_attention_backward, Q.device, stream, attention, _addr(Q), _addr(K), _addr(V), _addr(O), _addr(dO), _addr(lse),
+            _addr(q_offsets), _addr(q_lengths), _addr(k_offsets), _addr(k_lengths), _addr(dQ), _addr(dK), _addr(dV),
+            _addr(workspace), workspace.numel() * workspace.element_size())
+
+
+def make_qk_norm(Q, K, Y_Q, Y_K, rope_dim, eps=1e-6, theta=0.0):
+    """The description of norms and rotation of these tensors, [tokens, heads, d_head] each; K and Y_K may be None."""
+    q, yq = _rows("Q", Q), _rows("Y_Q", Y_Q, Q, Q.shape[1])
+    if Y_Q.shape[0] != Q.shape[0] or (K is None) != (Y_K is None) or (K is not None and (K.shape[0] != Q.shape[0] or Y_K.shape[0] != Q.shape[0])):
+        raise SwitchHeadError(SH_ERR_INVALID_ARG, "Q, K and the outputs must have the same number of rows")
+    k, yk, kv = (0, 0), (0, 0), 0
+    if K is not None:
+        k, yk, kv = _rows("K", K, Q), _rows("Y_K", Y_K, Q, K.shape[1]), K.shape[1]
+    return sh_qk_norm(Q.shape[0], Q.shape[1], kv, Q.shape[2], rope_dim, _dtype_code(Q), eps, theta, *q, *k, *yq, *yk)
+
+
+def switchhead_qk_norm_workspace_bytes(norm):
+    return int(lib().switchhead_qk_norm_workspace_bytes(norm))
+
+
+def switchhead_qk_norm_rope_forward(norm, Q, K, w_Q, w_K, positions, Y_Q, Y_K, stream=None):
+    _launch(lib().switchhead_qk_norm_rope_forward, Q.device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
+            _addr(Y_Q), _addr(Y_K))
+
+
+def switchhead_qk_norm_rope_backward(norm, Q, K, w_Q, w_K, positions, dY_Q, dY_K, dQ, dK, dw_Q, dw_K, workspace, stream=None):
+    _launch(lib().switchhead_qk_norm_rope_backward, Q.device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
+            _addr(dY_Q), _addr(dY_K), _addr(dQ), _addr(dK), _addr(dw_Q), _addr(dw_K),
+            _addr(workspace), workspace.numel() * workspace.element_size())

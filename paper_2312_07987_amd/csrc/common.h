@@ -375,6 +375,8 @@ void launch_router_bwd(const RouterBwdArgs& a, int bf16, hipStream_t s);
 // Step profiler (host.hip): when enabled, records an event on `st`; the time up to the next mark is
 // booked under `label` (a string literal; NULL closes the last step).
 void prof_mark(hipStream_t st, const char* label);
+// host.hip: sets the thread's last error and returns the status
+int report(int status, const char* text);
 // both routers' weights as bf16 [side][d_model][HEp], columns HE..HEp-1 zero (W1 unused when sides == 1)
 void launch_pack_router(const void* W0, const void* W1, void* Wp, int dm, int HE, int HEp, int sides, hipStream_t s);
 

@@ -64,6 +64,7 @@ void prof_mark_impl(hipStream_t st, const char* label) {
 }  // namespace
 
 void sh::prof_mark(hipStream_t st, const char* label) { prof_mark_impl(st, label); }
+int sh::report(int status, const char* text) { return fail((sh_status)status, "%s", text); }
 
 namespace {
 

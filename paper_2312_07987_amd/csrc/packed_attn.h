@@ -1,0 +1,329 @@
+// Attention over packed sequences with grouped heads (packed_fwd.hip, packed_few.hip, packed_bwd.hip): arguments, geometry, and the
+// operand helpers that let one kernel text serve bf16 and fp32 storage.
+//
+// Rows.  A sequence's queries of one kv head are the rows (token, head of the group): row = token * G + head % G.  All rows of a tile
+// read the same keys and values, whatever G is, so short sequences fill tiles G times better and the tile under a causal mask
+// ends at its last token.
+//
+// Slots.  The lengths are on the device, so the host launches an upper bound of the tiles: with tiles of BM rows sequence i owns the
+// slots from first(i) = floor(rows before i / BM) + i on, which are at least ceil(rows / BM) many before first(i + 1).  first() rises by
+// one or more, a wave finds the slot's sequence with one probe per lane and round (64 sequences one round, 4096 two).  At most one
+// slot per sequence is empty.
+//
+// Operands.  32 x 32 products over 16 reduction indices: lane = 32 g + r holds A[row r][k = 8 g .. 8 g + 7] and B[k][column r], register q of
+// the result is D[8 (q / 4) + 4 g + q % 4][column r].  fp32 takes the same 8 values per lane through eight 32x32x2 instructions (the i-th
+// multiplies k = i and k = 8 + i), so both types share every index below.
+#pragma once
+#include "mfma_util.h"
+
+namespace sh {
+
+struct PackedAttn {
+  const void *Q, *K, *V, *KP, *VP;
+  void* O;
+  float* lse;                          // [H][total_q] or NULL
+  const int *qoff, *qlen, *koff, *klen;   // qlen, klen may be NULL: the offsets' differences
+  int nseq, H, Hk, G, dh, causal, prefix, max_q;
+  int total_q, total_k;
+  long q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, kp_row, kp_head, vp_row, vp_head;
+  float scale;
+  unsigned g_inv;                      // div_magic(G)
+  // Key ranges that other work-groups take as well leave normalised fp32 rows and their log-sum-exp (natural logarithm, -inf: nothing seen):
+  // `dense` parts [part][total_q * H] and, from the few-row kernel, [slot * Hk + kv head][frows].
+  int nsplit, part0;                   // this launch's parts of the keys, the first one's number; nsplit 0: O is written
+  int flat, own;                       // flat: rows of all tokens over the prefix alone; own: the sequence's own keys alone
+  float *po, *pl;
+  int dhp;                             // part row length: dh rounded up to 4
+  int nparts;                          // dense parts in all (the joining kernel)
+  int chunk;                           // keys of a few-row work-group (0: all)
+  int frows;                           // rows of its parts: max_q * G
+  float *fo, *fl;
+};
+
+struct PackedAttnBwd {
+  PackedAttn f;
+  const void* dO;
+  const float* delta;                  // [H][total_q]
+  void *dQ, *dK, *dV;
+  void* dS;                            // score gradients [kv head][key][rows], bf16, or NULL: computed again
+  long ds_ld, ds_head;
+};
+
+struct SeqGeom {
+  int qbeg, lq, kbeg, lk;
+};
+__device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return min(max(v, lo), hi); }
+// (offsets and lengths come from device memory that the host has not seen: whatever they hold, every row stays inside the tensors)
+__device__ __forceinline__ SeqGeom seq_geom(const PackedAttn& a, int i) {
+  SeqGeom s;
+  s.qbeg = clamp_to(a.qoff[i], 0, a.total_q);
+  s.lq = clamp_to(a.qoff[i + 1], s.qbeg, a.total_q) - s.qbeg;
+  if (a.qlen) s.lq = clamp_to(a.qlen[i], 0, s.lq);
+  s.lq = min(s.lq, a.max_q);
+  s.kbeg = clamp_to(a.koff[i], 0, a.total_k);
+  s.lk = clamp_to(a.koff[i + 1], s.kbeg, a.total_k) - s.kbeg;
+  if (a.klen) s.lk = clamp_to(a.klen[i], 0, s.lk);
+  return s;
+}
+__device__ __forceinline__ int first_slot(const int* off, int total, int mul, int tile, int i) {
+  return (int)((unsigned)(clamp_to(off[i], 0, total) * mul) / (unsigned)tile) + i;
+}
+// The sequence of a slot and the slot's number within it; false for slots ahead of the first sequence.  All 64 lanes must take part.
+__device__ __forceinline__ bool find_slot(const int* off, int total, int nseq, int mul, int tile, int slot, int& seq, int& nth) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = nseq, first = 0;
+  bool any = true;
+  do {
+    const int step = (n + 63) >> 6;
+    const int i = lo + min(lane * step, n - 1);
+    const int f = first_slot(off, total, mul, tile, i);
+    const unsigned long long m = __ballot(lane * step < n && f <= slot);
+    any = m != 0;
+    const int k = any ? __popcll(m) - 1 : 0;
+    first = __shfl(f, k, 64);
+    lo += k * step;
+    n = min(step, n - k * step);
+  } while (any && n > 1);
+  seq = __builtin_amdgcn_readfirstlane(lo);
+  nth = __builtin_amdgcn_readfirstlane(slot - first);
+  return any;
+}
+
+// ---- 16-byte pieces of rows -----------------------------------------------------------------------------------------------
+// AL: alignment in bytes of every row (16, 8, or the element): how a piece may be read and written.
+template <typename T>
+struct Elem;
+template <>
+struct Elem<bf16_t> {
+  typedef unsigned short raw;
+  static constexpr int PER = 8;
+};
+template <>
+struct Elem<float> {
+  typedef float raw;
+  static constexpr int PER = 4;
+};
+
+// The piece at element d of a row of dh elements; what lies past dh is read from inside the row and cut off by cut_piece.
+template <typename T, int AL>
+__device__ __forceinline__ uint4 load_row_piece(const typename Elem<T>::raw* row, int d, int dh) {
+  if constexpr (AL == 16) {
+    return *(const uint4*)(row + (d < dh ? d : 0));
+  } else if constexpr (AL == 8) {
+    constexpr int H = Elem<T>::PER / 2;
+    const uint2 lo = *(const uint2*)(row + (d < dh ? d : 0)), hi = *(const uint2*)(row + (d + H < dh ? d + H : 0));
+    return make_uint4(lo.x, lo.y, hi.x, hi.y);
+  } else if constexpr (sizeof(T) == 2) {
+    unsigned w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const unsigned lo = row[d + 2 * j < dh ? d + 2 * j : 0], hi = row[d + 2 * j + 1 < dh ? d + 2 * j + 1 : 0];
+      w[j] = lo | hi << 16;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  } else {
+    unsigned w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(row[d + j < dh ? d + j : 0]);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+template <typename T, int AL>
+__device__ __forceinline__ uint4 cut_piece(uint4 v, int d, int dh) {
+  if constexpr (AL == 16) {
+    if (d >= dh) v = make_uint4(0, 0, 0, 0);
+  } else {
+    constexpr int PW = 4 / sizeof(T);   // elements of a word
+    unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (d + j * PW >= dh) w[j] = 0;
+      if constexpr (AL < 4) {
+        if (d + j * PW + 1 >= dh) w[j] &= 0xffffu;
+      }
+    }
+    v = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  return v;
+}
+
+// NROWS rows on their way from memory to LDS.  load() carries no tests: a row past the last valid one repeats it and a column past dh
+// repeats column 0; store() puts zeros in both places (a key that no query sees has probability 0, and 0 times what lies behind a
+// sequence need not be 0).
+template <typename T, int DH, int AL, int NROWS, int NT>
+struct PieceTile {
+  typedef typename Elem<T>::raw raw;
+  static constexpr int PER = Elem<T>::PER, CPR = DH / PER, TOTAL = NROWS * CPR, NCH = (TOTAL + NT - 1) / NT;
+  uint4 r[NCH];
+  __device__ __forceinline__ void load(const raw* src, long row_stride, int valid, int dh, int tid) {
+    if (valid <= 0) return;   // uniform
+    const int last = min(valid, NROWS) - 1;
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = tid + i * NT;
+      r[i] = load_row_piece<T, AL>((const raw*)((const char*)src + (unsigned)min(c / CPR, last) * (unsigned)row_stride * (unsigned)sizeof(raw)), c % CPR * PER, dh);
+    }
+  }
+  __device__ __forceinline__ void store(raw* t, int ld, int valid, int dh, int tid) const {
+    const bool whole = valid >= NROWS && dh == DH;   // uniform
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = tid + i * NT;
+      if (TOTAL % NT != 0 && c >= TOTAL) continue;
+      const int row = c / CPR, d = c % CPR * PER;
+      uint4 v = r[i];
+      if (!whole) {
+        v = cut_piece<T, AL>(v, d, dh);
+        if (row >= valid) v = make_uint4(0, 0, 0, 0);
+      }
+      *(uint4*)(t + row * ld + d) = v;
+    }
+  }
+};
+
+// ---- operand fragments ----------------------------------------------------------------------------------------------------
+struct f32x8 {
+  f32x4 lo, hi;
+};
+template <typename T>
+struct FragOf;
+template <>
+struct FragOf<bf16_t> {
+  typedef bf16x8 type;
+};
+template <>
+struct FragOf<float> {
+  typedef f32x8 type;
+};
+template <typename T>
+using frag_t = typename FragOf<T>::type;
+
+// LDS row stride: 16-byte fragment reads of 8 rows fall on all banks, and so do the rows that a transposing read (bf16) or the two lane
+// halves' column reads (fp32) touch at a time
+template <typename T, int DH>
+constexpr int tile_ld() {
+  return sizeof(T) == 2 ? DH + 16 : DH + 8;
+}
+
+__device__ __forceinline__ bf16x8 row_frag(const unsigned short* p) { return *(const bf16x8*)p; }
+__device__ __forceinline__ f32x8 row_frag(const float* p) { return f32x8{*(const f32x4*)p, *(const f32x4*)(p + 4)}; }
+
+// rows k0 .. k0 + 3 and k1 .. k1 + 3 of column nb + lane % 32 of a tile stored [row][column]
+__device__ __forceinline__ bf16x8 col_frag(const unsigned short* tile, int ld, int k0, int k1, int nb, int lane) {
+  const int s = lane & 15, col = nb + ((lane >> 4) & 1) * 16 + (s & 3) * 4;
+  union {
+    s16x4 half[2];
+    bf16x8 v;
+  } u;
+  u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, tile + (k0 + (s >> 2)) * ld + col));
+  u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, tile + (k1 + (s >> 2)) * ld + col));
+  return u.v;
+}
+__device__ __forceinline__ f32x8 col_frag(const float* tile, int ld, int k0, int k1, int nb, int lane) {
+  const float* p = tile + nb + (lane & 31);
+  f32x8 f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    f.lo[j] = p[(k0 + j) * ld];
+    f.hi[j] = p[(k1 + j) * ld];
+  }
+  return f;
+}
+
+// elements d .. d + 7 of a row in memory, zeros from dh on; zeros altogether for a row that is not there
+template <typename T, int AL>
+__device__ __forceinline__ frag_t<T> mem_frag(const typename Elem<T>::raw* row, int d, int dh, bool valid) {
+  union {
+    uint4 q[sizeof(T) / 2];
+    frag_t<T> v;
+  } u;
+#pragma unroll
+  for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+    u.q[j] = make_uint4(0, 0, 0, 0);
+    if (valid) u.q[j] = cut_piece<T, AL>(load_row_piece<T, AL>(row, d + j * Elem<T>::PER, dh), d + j * Elem<T>::PER, dh);
+  }
+  return u.v;
+}
+
+__device__ __forceinline__ void pack_frag(bf16x8& o, const float* v) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
+}
+__device__ __forceinline__ void pack_frag(f32x8& o, const float* v) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    o.lo[i] = v[i];
+    o.hi[i] = v[4 + i];
+  }
+}
+
+__device__ __forceinline__ f32x16 mma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 mma32(f32x8 a, f32x8 b, f32x16 c) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.lo[i], b.lo[i], c, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.hi[i], b.hi[i], c, 0, 0, 0);
+  return c;
+}
+
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+
+// acc[d] holds X^T[32 d + 8 (i / 4) + 4 g + i % 4][this lane's row]: stores them to that row
+template <typename T, int AL, int NDB>
+__device__ __forceinline__ void store_row(typename Elem<T>::raw* dst, const f32x16* acc, float mul, int g, int dh) {
+#pragma unroll
+  for (int d = 0; d < NDB; ++d)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      const int dd = d * 32 + 8 * i4 + 4 * g;
+      const float x0 = acc[d][4 * i4] * mul, x1 = acc[d][4 * i4 + 1] * mul, x2 = acc[d][4 * i4 + 2] * mul, x3 = acc[d][4 * i4 + 3] * mul;
+      if constexpr (sizeof(T) == 2 && AL >= 8) {
+        if (dd < dh) *(uint2*)(dst + dd) = make_uint2(pack_bf16x2(x0, x1), pack_bf16x2(x2, x3));
+      } else if constexpr (sizeof(T) == 4 && AL == 16) {
+        if (dd < dh) *(float4*)(dst + dd) = make_float4(x0, x1, x2, x3);
+      } else {
+        const float x[4] = {x0, x1, x2, x3};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (dd + j < dh) st((T*)dst, dd + j, x[j]);
+      }
+    }
+}
+
+// Norms and rotation of queries (0) and keys (1): qk_norm.hip
+struct QkNormArgs {
+  const void* x[2];
+  const void* w[2];        // [dh] or NULL: ones
+  const int* positions;    // [tokens] or NULL: the token's index
+  void* y[2];
+  const void* dy[2];
+  void* dx[2];
+  float* dw[2];
+  float* part;             // [work-groups][2][dh]
+  long tokens, x_row[2], x_head[2], y_row[2], y_head[2];   // gradients lie as their tensors do
+  int H[2], dh, rope_dim, hchunk;
+  float eps;
+  double rate[7];          // theta^(-2 2^k / rope_dim)
+};
+struct QkNormGrid {
+  int x, y, hchunk;
+};
+QkNormGrid qk_norm_grid(long tokens, int heads, int dh, int bf16);
+void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipStream_t s);
+
+// launchers
+void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s);
+void launch_packed_few(const PackedAttn& a, int bf16, int align, hipStream_t s);
+void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s);
+void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta, hipStream_t s);
+
+enum { PACKED_BM = 128, PACKED_FEW = 16 };
+// slots of `rows` rows in tiles of bm over nseq sequences
+static inline long packed_slots(long rows, int bm, int nseq) { return rows / bm + nseq; }
+
+}  // namespace sh
