@@ -113,7 +113,7 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
     // Chunks that make some 1500 work-groups of the keys there are; where a sequence's keys are few, one work-group takes them all
     const long keys = (long)a.max_k * seqs < a.total_k ? (long)a.max_k * seqs : a.total_k;
     long chunk = ceil_div(keys * a.nkv_heads, 1536);
-    chunk = ceil_div(chunk < 256 ? 256 : chunk > 4096 ? 4096 : chunk, 128) * 128;
+    chunk = ceil_div(chunk < 256 ? 256 : chunk > 1024 ? 1024 : chunk, 128) * 128;
     if (a.max_k > 2 * chunk || (a.max_k > chunk && seqs * a.nkv_heads < 256)) p.chunk = (int)chunk;
   } else {
     // Few tiles and many keys: several work-groups share a tile's keys
@@ -150,8 +150,46 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   return SH_OK;
 }
 
-// Workspace of a backward pass: delta, and the score gradients where they are kept
-size_t backward_bytes(const AttnPlan& p) { return align_up((size_t)p.a.total_q * p.a.nheads * 4) + 256; }
+// Workspace of a backward pass: delta, the parts of dK and dV, and the score gradients where they are kept
+struct BwdPlan {
+  size_t dkv, ds, total;   // ds 0: not kept
+  int rchunk, rparts;
+  long ds_ld, dkv_floats;
+};
+constexpr size_t MAX_DS_BYTES = (size_t)2 << 30;
+BwdPlan plan_backward(const AttnPlan& p) {
+  const sh_attention& a = p.a;
+  BwdPlan b{};
+  const long rows = (long)a.max_q * p.G, w = packed_width(a.d_head);
+  size_t off = align_up((size_t)a.total_q * a.nheads * 4) + 256;
+  b.rchunk = (int)(rows > 0 ? (rows + 31) / 32 * 32 : 32);
+  b.rparts = 1;
+  if (a.dtype == SH_BF16 && a.d_head <= 128 && rows > 0) {
+    // Rows of a dK / dV work-group: about what a CU gets if the key tiles, a third of a rectangle of the longest rows each, were dealt evenly,
+    // so that no work-group is much longer than that; at least 512, where a work-group is about as long as its start and the extra parts.
+    const long tiles = ceil_div(a.total_k, PACKED_KB) * a.nkv_heads;
+    long chunk = tiles * rows * 35 / 100 / 256;
+    chunk = ceil_div(chunk < 512 ? 512 : chunk, 32) * 32;
+    if (chunk < rows) {
+      b.rparts = (int)ceil_div(rows, chunk);
+      b.rchunk = (int)(ceil_div(ceil_div(rows, b.rparts), 32) * 32);
+      b.rparts = (int)ceil_div(rows, b.rchunk);
+    }
+    if (b.rparts > 1) {
+      b.dkv = off;
+      b.dkv_floats = 2l * PACKED_KB * w;
+      off += align_up((size_t)b.rparts * packed_slots(a.total_k, PACKED_KB, a.nseq) * a.nkv_heads * b.dkv_floats * 4);
+    }
+    b.ds_ld = ceil_div(rows, PACKED_BM) * PACKED_BM;
+    const size_t ds = (size_t)a.nkv_heads * a.total_k * b.ds_ld * 2;
+    if (ds > 0 && ds <= MAX_DS_BYTES) {
+      b.ds = off;
+      off += align_up(ds);
+    }
+  }
+  b.total = off;
+  return b;
+}
 
 sh_status check_workspace(const void* ws, size_t have, size_t need) {
   if (!ws) return fail(SH_ERR_INVALID_ARG, "workspace is NULL");
@@ -251,7 +289,7 @@ extern "C" {
 size_t switchhead_attention_workspace_bytes(const sh_attention* d, int32_t backward) {
   AttnPlan p;
   if (plan_attention(p, d) != SH_OK) return 0;
-  const size_t b = backward ? backward_bytes(p) : 0;
+  const size_t b = backward ? plan_backward(p).total : 0;
   return b > p.total ? b : p.total;
 }
 
@@ -333,7 +371,8 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
   if (!disjoint(s.total_q, s.nheads, s.q_row, s.q_head, s.d_head) || !disjoint(s.total_k, s.nkv_heads, s.k_row, s.k_head, s.d_head) ||
       !disjoint(s.total_k, s.nkv_heads, s.v_row, s.v_head, s.d_head))
     return fail(SH_ERR_INVALID_ARG, "the strides of Q, K or V lay the rows of a gradient over each other");
-  if ((r = check_workspace(workspace, workspace_bytes, backward_bytes(p))) != SH_OK) return r;
+  const BwdPlan w = plan_backward(p);
+  if ((r = check_workspace(workspace, workspace_bytes, w.total)) != SH_OK) return r;
   if (s.nseq == 0 || (s.total_q == 0 && s.total_k == 0)) return SH_OK;
   const hipStream_t st = (hipStream_t)hip_stream;
   const int bf16 = s.dtype == SH_BF16;
@@ -351,6 +390,12 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
   b.dV = dV;
   float* delta = (float*)workspace;
   b.delta = delta;
+  b.rchunk = w.rchunk;
+  b.rparts = w.rparts;
+  b.dkv = (float*)((char*)workspace + w.dkv);
+  b.dkv_floats = w.dkv_floats;
+  b.ds_ld = w.ds_ld;
+  b.dS = w.ds ? (char*)workspace + w.ds : nullptr;
   launch_packed_bwd(b, bf16, align, delta, st);
   prof_mark(st, nullptr);
   return check_launch("switchhead_attention_backward");

@@ -45,8 +45,14 @@ struct PackedAttnBwd {
   const void* dO;
   const float* delta;                  // [H][total_q]
   void *dQ, *dK, *dV;
-  void* dS;                            // score gradients [kv head][key][rows], bf16, or NULL: computed again
-  long ds_ld, ds_head;
+  // bf16, head widths 33 .. 128: score gradients dS^T [kv head][key][row of the sequence], rows of ds_ld, or NULL: computed again for dQ
+  void* dS;
+  long ds_ld;
+  // rows of a dK / dV work-group (a multiple of 32): key tiles that see more leave fp32 parts, [part][slot * Hk + kv head][dV, dK] of
+  // dkv_floats each, for a second kernel
+  int rchunk, rparts;
+  float* dkv;
+  long dkv_floats;
 };
 
 struct SeqGeom {
@@ -68,25 +74,34 @@ __device__ __forceinline__ SeqGeom seq_geom(const PackedAttn& a, int i) {
 __device__ __forceinline__ int first_slot(const int* off, int total, int mul, int tile, int i) {
   return (int)((unsigned)(clamp_to(off[i], 0, total) * mul) / (unsigned)tile) + i;
 }
-// The sequence of a slot and the slot's number within it; false for slots ahead of the first sequence.  All 64 lanes must take part.
-__device__ __forceinline__ bool find_slot(const int* off, int total, int nseq, int mul, int tile, int slot, int& seq, int& nth) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, n = nseq, first = 0;
-  bool any = true;
-  do {
+// The sequence of a slot, the slot's number within it and the sequence's places; false for slots ahead of the first sequence.  KEYS: slots of
+// `tile` keys, else of `tile` rows of G per query.  In the last round, where the lanes' sequences are neighbours, every lane reads its
+// sequence's places along with the offset, so that up to 64 sequences cost one trip to memory.  All 64 lanes must take part.
+template <bool KEYS>
+__device__ __forceinline__ bool find_slot(const PackedAttn& a, int tile, int slot, int& nth, SeqGeom& s) {
+  const int* off = KEYS ? a.koff : a.qoff;
+  const int total = KEYS ? a.total_k : a.total_q, mul = KEYS ? 1 : a.G, lane = threadIdx.x & 63;
+  int lo = 0, n = a.nseq;
+  while (n > 64) {
     const int step = (n + 63) >> 6;
-    const int i = lo + min(lane * step, n - 1);
-    const int f = first_slot(off, total, mul, tile, i);
-    const unsigned long long m = __ballot(lane * step < n && f <= slot);
-    any = m != 0;
-    const int k = any ? __popcll(m) - 1 : 0;
-    first = __shfl(f, k, 64);
+    const unsigned long long m = __ballot(lane * step < n && first_slot(off, total, mul, tile, lo + min(lane * step, n - 1)) <= slot);
+    if (!m) return false;
+    const int k = __popcll(m) - 1;
     lo += k * step;
     n = min(step, n - k * step);
-  } while (any && n > 1);
-  seq = __builtin_amdgcn_readfirstlane(lo);
-  nth = __builtin_amdgcn_readfirstlane(slot - first);
-  return any;
+  }
+  const int i = lo + min(lane, n - 1);
+  const int f = first_slot(off, total, mul, tile, i);
+  const SeqGeom mine = seq_geom(a, i);
+  const unsigned long long m = __ballot(lane < n && f <= slot);
+  if (!m) return false;
+  const int k = __builtin_amdgcn_readfirstlane(__popcll(m) - 1);
+  nth = slot - __builtin_amdgcn_readlane(f, k);
+  s.qbeg = __builtin_amdgcn_readlane(mine.qbeg, k);
+  s.lq = __builtin_amdgcn_readlane(mine.lq, k);
+  s.kbeg = __builtin_amdgcn_readlane(mine.kbeg, k);
+  s.lk = __builtin_amdgcn_readlane(mine.lk, k);
+  return true;
 }
 
 // ---- 16-byte pieces of rows -----------------------------------------------------------------------------------------------
@@ -322,7 +337,9 @@ void launch_packed_few(const PackedAttn& a, int bf16, int align, hipStream_t s);
 void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s);
 void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta, hipStream_t s);
 
-enum { PACKED_BM = 128, PACKED_FEW = 16 };
+enum { PACKED_BM = 128, PACKED_FEW = 16, PACKED_KB = 128 };
+// head width that a work-group's tiles are laid out for
+static inline int packed_width(int dh) { return dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
 // slots of `rows` rows in tiles of bm over nseq sequences
 static inline long packed_slots(long rows, int bm, int nseq) { return rows / bm + nseq; }
 

@@ -5,23 +5,34 @@
 
 namespace sh {
 
-// delta[head][token]: a wave takes one (token, head) per 16, 32 or 64 lanes
-template <typename T, int LR>
+typedef unsigned short raw16;
+
+// delta[head][token] = <dO, O>, from the rows as they are stored: LR lanes hold a row in 16-byte pieces.  (O's rounding is an error of
+// P delta that dS = P (dP - delta) shares with the plain form's rounded O; dS is rounded once more on its way into the products.)
+template <typename T, int LR, int AL>
 __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn a, const void* dO_, float* delta) {
   typedef typename Elem<T>::raw raw;
-  const int sub = threadIdx.x / LR, c = threadIdx.x % LR * 4;
-  const long id = (long)blockIdx.x * (256 / LR) + sub;
+  const int d = threadIdx.x % LR * Elem<T>::PER;
+  const long id = (long)blockIdx.x * (256 / LR) + threadIdx.x / LR;
   if (id >= (long)a.total_q * a.H) return;
-  const int tok = (int)(id / a.H), head = (int)(id % a.H);
-  const T* O = (const T*)((const raw*)a.O + (long)tok * a.o_row + (long)head * a.o_head);
-  const T* dO = (const T*)((const raw*)dO_ + (long)tok * a.o_row + (long)head * a.o_head);
+  const int tok = (int)(id / a.H), head = (int)(id - (long)tok * a.H);
+  const long at = (long)tok * a.o_row + (long)head * a.o_head;
+  const uint4 o = cut_piece<T, AL>(load_row_piece<T, AL>((const raw*)a.O + at, d, a.dh), d, a.dh);
+  const uint4 g = cut_piece<T, AL>(load_row_piece<T, AL>((const raw*)dO_ + at, d, a.dh), d, a.dh);
+  const unsigned ow[4] = {o.x, o.y, o.z, o.w}, gw[4] = {g.x, g.y, g.z, g.w};
   float x = 0.f;
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    if (c + j < a.dh) x += ld(O, c + j) * ld(dO, c + j);
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (sizeof(T) == 2) {
+      x = fmaf(__uint_as_float(ow[j] << 16), __uint_as_float(gw[j] << 16), x);
+      x = fmaf(__uint_as_float(ow[j] & 0xffff0000u), __uint_as_float(gw[j] & 0xffff0000u), x);
+    } else {
+      x = fmaf(__uint_as_float(ow[j]), __uint_as_float(gw[j]), x);
+    }
+  }
 #pragma unroll
-  for (int d = 1; d < LR; d <<= 1) x += __shfl_xor(x, d, 64);
-  if (c == 0) delta[(long)head * a.total_q + tok] = x;
+  for (int k = 1; k < LR; k <<= 1) x += __shfl_xor(x, k, 64);
+  if (d == 0) delta[(long)head * a.total_q + tok] = x;
 }
 
 // dK and dV of 128 keys of one (sequence, kv head): 4 waves x 32 keys, whose K and V rows are registers; tiles of 32 rows of Q and dO go
@@ -38,9 +49,9 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
 
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
-  int seq, nth;
-  if (!find_slot(a.koff, a.total_k, a.nseq, 1, KB, slot, seq, nth)) return;
-  const SeqGeom s = seq_geom(a, seq);
+  int nth;
+  SeqGeom s;
+  if (!find_slot<true>(a, KB, slot, nth, s)) return;
   const int k0 = nth * KB;
   if (k0 >= s.lk) return;
   const int off = s.lk - s.lq, rows = s.lq * a.G, key = k0 + wave * 32 + r;
@@ -143,6 +154,318 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
   }
 }
 
+// The same for bf16 heads of 33 .. 128 elements with two kinds of waves.  A single wave per SIMD, which is all that the kernel above has registers
+// for, leaves the matrix cores idle during exponentials, conversions and LDS traffic.  Here waves 0 .. 3 (score) hold the K and V fragments
+// of 32 keys each, form P and dS of a tile of 32 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
+// 4 .. 7 (gradient) hold the dK and dV accumulators of the same keys, add the previous tile's products, and move the row tiles from memory to
+// LDS.  One of each kind per SIMD; three stages for the row tiles (written a trip ahead, read by the score waves in the next
+// trip and by the gradient waves in the one after), two buffers for the fragments, one barrier per trip.
+// Under a causal mask the first keys of a sequence are seen by all of its rows, the last by few, so rows are cut into ranges of rchunk
+// and a (key tile, range) is a work-group; ranges that are the only one of their tile write dK and dV, others fp32 parts.
+template <int DH, int AL>
+__global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) {
+  const PackedAttn& a = b.f;
+  constexpr int QT = 32, KB = PACKED_KB, NST = 3, LD = DH + 16, NKD = DH / 16, NDB = DH / 32, CPR = DH / 8, TOTAL = QT * CPR, NCH = (TOTAL + 255) / 256;
+  constexpr int STAGE = 2 * QT * LD;
+  __shared__ __attribute__((aligned(16))) unsigned short tiles[NST * STAGE];
+  __shared__ __attribute__((aligned(16))) uint4 hand[2][4][4][64];   // [buffer][key block][P st 0, P st 1, dS st 0, dS st 1][lane]
+  __shared__ __attribute__((aligned(16))) float lse_s[NST][QT], del_s[NST][QT];
+
+  int bid = blockIdx.x;
+  const int hk = bid % a.Hk;
+  bid /= a.Hk;
+  const int part = bid % b.rparts, slot = bid / b.rparts;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, blk = wave & 3, r = lane & 31, g = lane >> 5, dh = a.dh;
+  int nth;
+  SeqGeom s;
+  if (!find_slot<true>(a, KB, slot, nth, s)) return;
+  const int k0 = nth * KB;
+  if (k0 >= s.lk) return;
+  const int off = s.lk - s.lq, rows = s.lq * a.G, key = k0 + blk * 32 + r, wk_first = k0 + blk * 32;
+  const int first = a.causal ? max(k0 - off, 0) * a.G / QT * QT : 0;   // the first row tile that sees one of the keys
+  // this range of the rows, and whether it is the only one
+  const int p0 = min(first, max(rows - 1, 0)) / b.rchunk, p1 = max(rows - 1, 0) / b.rchunk;
+  if (part < p0 || part > p1) return;
+  const int rbeg = max(first, part * b.rchunk), rend = min(rows, (part + 1) * b.rchunk);
+  const int n = rbeg < rend ? (rend - rbeg + QT - 1) / QT : 0;
+
+  if (wave < 4) {
+    bf16x8 kf[NKD], vf[NKD];
+    const unsigned short* K = (const unsigned short*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head;
+    const unsigned short* V = (const unsigned short*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head;
+#pragma unroll
+    for (int kk = 0; kk < NKD; ++kk) {
+      kf[kk] = mem_frag<bf16_t, AL>(K, kk * 16 + 8 * g, dh, key < s.lk);
+      vf[kk] = mem_frag<bf16_t, AL>(V, kk * 16 + 8 * g, dh, key < s.lk);
+    }
+    // (keys past the sequence have no row of dS^T: they repeat the last key's address and do not store)
+    unsigned short* dsrow = nullptr;
+    if (b.dS) dsrow = (unsigned short*)b.dS + ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 4 * g;
+    const bool ds_store = b.dS && key < s.lk;
+    const float sc = a.scale * 1.44269504088896340736f;
+    for (int it = 0; it <= n; ++it) {
+      __syncthreads();
+      if (it == n) break;
+      const int r0 = rbeg + it * QT;
+      const unsigned short* Qr = tiles + (it % NST) * STAGE;
+      const unsigned short* Gr = Qr + QT * LD;
+      f32x16 S = zero16(), dP = zero16();
+#pragma unroll
+      for (int kk = 0; kk < NKD; ++kk) {
+        S = mma32(row_frag(&Qr[r * LD + kk * 16 + 8 * g]), kf[kk], S);
+        dP = mma32(row_frag(&Gr[r * LD + kk * 16 + 8 * g]), vf[kk], dP);
+      }
+      float p[16], ds[16];
+      const float* Ls = lse_s[it % NST];
+      const float* Ds = del_s[it % NST];
+      // wave-uniform: most tiles lie wholly inside the visible region
+      const bool masked = r0 + QT > rend || wk_first + 32 > s.lk || (a.causal && wk_first + 31 > div_by(r0, a.g_inv) + off);
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 L = *(const f32x4*)&Ls[8 * i4 + 4 * g], D = *(const f32x4*)&Ds[8 * i4 + 4 * g];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int i = 4 * i4 + t;
+          p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L[t]));
+          ds[i] = p[i] * (dP[i] - D[t]);
+        }
+      }
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int rr = r0 + 8 * (i >> 2) + 4 * g + (i & 3);
+          const bool vis = rr < rend && key < s.lk && (!a.causal || key <= div_by(rr, a.g_inv) + off);
+          p[i] = vis ? p[i] : 0.f;
+          ds[i] = vis ? ds[i] : 0.f;
+        }
+      }
+      uint4* hd = hand[it & 1][blk][0] + lane;
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        union {
+          bf16x8 v;
+          uint4 q;
+          uint2 hh[2];
+        } up, ud;
+        pack_frag(up.v, &p[8 * st]);
+        pack_frag(ud.v, &ds[8 * st]);
+        hd[st * 64] = up.q;
+        hd[(2 + st) * 64] = ud.q;
+        if (ds_store) {   // elements 0..3 / 4..7: rows r0 + 16 st + 4 g + {0..3} / + 8 + {0..3} of this lane's key
+          *(uint2*)(dsrow + r0 + 16 * st) = ud.hh[0];
+          *(uint2*)(dsrow + r0 + 16 * st + 8) = ud.hh[1];
+        }
+      }
+    }
+    return;
+  }
+
+  const int gt = tid - 256;
+  uint4 tq[NCH], tg[NCH];
+  float nlse = 0.f, ndel = 0.f;
+  auto prefetch = [&](int r0) {   // (rows past the end repeat the last one)
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = gt + i * 256, row = min(r0 + c / CPR, rows - 1), d = c % CPR * 8;
+      const int tok = div_by(row, a.g_inv), head = hk * a.G + row - tok * a.G;
+      tq[i] = load_row_piece<bf16_t, AL>((const unsigned short*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head, d, dh);
+      tg[i] = load_row_piece<bf16_t, AL>((const unsigned short*)b.dO + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head, d, dh);
+    }
+    const int row = min(r0 + (gt & (QT - 1)), rows - 1), tok = div_by(row, a.g_inv), head = hk * a.G + row - tok * a.G;
+    nlse = a.lse[(long)head * a.total_q + s.qbeg + tok];
+    ndel = b.delta[(long)head * a.total_q + s.qbeg + tok];
+  };
+  auto stage = [&](int st, int r0) {
+    unsigned short* t = tiles + st * STAGE;
+    const bool whole = r0 + QT <= rows && dh == DH;   // uniform
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      const int c = gt + i * 256, row = c / CPR, d = c % CPR * 8;
+      if (TOTAL % 256 != 0 && c >= TOTAL) continue;
+      uint4 q = tq[i], x = tg[i];
+      if (!whole) {
+        q = cut_piece<bf16_t, AL>(q, d, dh);
+        x = cut_piece<bf16_t, AL>(x, d, dh);
+        if (r0 + row >= rows) q = x = make_uint4(0, 0, 0, 0);
+      }
+      *(uint4*)(t + row * LD + d) = q;
+      *(uint4*)(t + (QT + row) * LD + d) = x;
+    }
+    if (gt < QT) {
+      lse_s[st][gt] = nlse * 1.44269504088896340736f;
+      del_s[st][gt] = ndel;
+    }
+  };
+  f32x16 accK[NDB], accV[NDB];
+#pragma unroll
+  for (int d = 0; d < NDB; ++d) accK[d] = accV[d] = zero16();
+  if (n > 0) {
+    prefetch(rbeg);
+    stage(0, rbeg);
+    if (n > 1) prefetch(rbeg + QT);
+  }
+  for (int it = 0; it <= n; ++it) {
+    __syncthreads();
+    // the tile it + 1 (requested a trip ago) goes into its stage and the tile it + 2 starts to travel
+    if (it + 1 < n) {
+      stage((it + 1) % NST, rbeg + (it + 1) * QT);
+      if (it + 2 < n) prefetch(rbeg + (it + 2) * QT);
+    }
+    if (it == 0) continue;
+    const unsigned short* Qt = tiles + ((it - 1) % NST) * STAGE;
+    const unsigned short* Gt = Qt + QT * LD;
+    const uint4* hd = hand[(it - 1) & 1][blk][0] + lane;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      union {
+        uint4 q;
+        bf16x8 v;
+      } up, ud;
+      up.q = hd[st * 64];
+      ud.q = hd[(2 + st) * 64];
+      const int kb0 = 16 * st + 4 * g;
+#pragma unroll
+      for (int d = 0; d < NDB; ++d) {
+        accV[d] = mma32(col_frag(Gt, LD, kb0, kb0 + 8, d * 32, lane), up.v, accV[d]);
+        accK[d] = mma32(col_frag(Qt, LD, kb0, kb0 + 8, d * 32, lane), ud.v, accK[d]);
+      }
+    }
+  }
+  if (p0 == p1) {
+    if (key < s.lk) {
+      store_row<bf16_t, AL, NDB>((unsigned short*)b.dK + (long)(s.kbeg + key) * a.k_row + (long)hk * a.k_head, accK, a.scale, g, dh);
+      store_row<bf16_t, AL, NDB>((unsigned short*)b.dV + (long)(s.kbeg + key) * a.v_row + (long)hk * a.v_head, accV, 1.f, g, dh);
+    }
+    return;
+  }
+  // a part: accumulators in register order, 16 bytes per lane
+  f32x4* out = (f32x4*)(b.dkv + ((long)part * gridDim.x / b.rparts + (long)slot * a.Hk + hk) * b.dkv_floats) + blk * NDB * 4 * 64 + lane;
+#pragma unroll
+  for (int d = 0; d < NDB; ++d)
+#pragma unroll
+    for (int i4 = 0; i4 < 4; ++i4) {
+      out[(d * 4 + i4) * 64] = f32x4{accV[d][4 * i4], accV[d][4 * i4 + 1], accV[d][4 * i4 + 2], accV[d][4 * i4 + 3]};
+      out[(4 * NDB * 4 + d * 4 + i4) * 64] = f32x4{accK[d][4 * i4], accK[d][4 * i4 + 1], accK[d][4 * i4 + 2], accK[d][4 * i4 + 3]};
+    }
+}
+
+// Adds the parts of the key tiles that have several, in range order: waves 0 .. 3 dV, 4 .. 7 dK, 32 keys each
+template <int DH, int AL>
+__global__ __launch_bounds__(512) void packed_dkv_join_kernel(PackedAttnBwd b) {
+  const PackedAttn& a = b.f;
+  constexpr int NDB = DH / 32;
+  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blk = wave & 3, r = lane & 31, g = lane >> 5, dh = a.dh;
+  int nth;
+  SeqGeom s;
+  if (!find_slot<true>(a, PACKED_KB, slot, nth, s)) return;
+  const int k0 = nth * PACKED_KB;
+  if (k0 >= s.lk) return;
+  const int off = s.lk - s.lq, rows = s.lq * a.G, first = a.causal ? max(k0 - off, 0) * a.G / 32 * 32 : 0;
+  const int p0 = min(first, max(rows - 1, 0)) / b.rchunk, p1 = max(rows - 1, 0) / b.rchunk;
+  if (p0 == p1) return;
+  f32x16 acc[NDB];
+#pragma unroll
+  for (int d = 0; d < NDB; ++d) acc[d] = zero16();
+  for (int p = p0; p <= p1; ++p) {
+    const f32x4* in = (const f32x4*)(b.dkv + ((long)p * gridDim.x + (long)slot * a.Hk + hk) * b.dkv_floats) + ((wave >= 4 ? 4 : 0) + blk) * NDB * 4 * 64 + lane;
+#pragma unroll
+    for (int d = 0; d < NDB; ++d)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        const f32x4 v = in[(d * 4 + i4) * 64];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[d][4 * i4 + j] += v[j];
+      }
+  }
+  const int key = k0 + blk * 32 + r;
+  if (key >= s.lk) return;
+  if (wave < 4)
+    store_row<bf16_t, AL, NDB>((unsigned short*)b.dV + (long)(s.kbeg + key) * a.v_row + (long)hk * a.v_head, acc, 1.f, g, dh);
+  else
+    store_row<bf16_t, AL, NDB>((unsigned short*)b.dK + (long)(s.kbeg + key) * a.k_row + (long)hk * a.k_head, acc, a.scale, g, dh);
+}
+
+// dQ from the kept score gradients: dQ^T[d][row] = s sum_key K^T[d][key] dS^T[key][row], a plain product.  128 rows of one (sequence, kv head),
+// tiles of 64 keys of K and of dS^T through LDS, both read by columns; a wave owns 64 rows and half of d (96: 32 rows and all of d).
+// What the dK / dV work-groups of a key tile did not write (rows that see none of its keys) is replaced by zeros.
+template <int DH, int AL>
+__global__ __launch_bounds__(256, 2) void packed_dq_ds_kernel(PackedAttnBwd b) {
+  const PackedAttn& a = b.f;
+  constexpr int KT = 64, LD = DH + 16, BM = PACKED_BM, LDD = BM + 16, NDB = DH / 32, NP = KT * BM / 8 / 256;
+  constexpr bool SPLIT = NDB % 2 == 0;
+  constexpr int NJ = SPLIT ? 2 : 1, ND = SPLIT ? NDB / 2 : NDB;
+  __shared__ __attribute__((aligned(16))) unsigned short Ks[KT * LD], Ds[KT * LDD];
+  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
+  int nth;
+  SeqGeom s;
+  if (!find_slot<false>(a, BM, slot, nth, s)) return;
+  const int rows = s.lq * a.G, nt = (rows + BM - 1) / BM;
+  if (nth >= nt) return;
+  const int row0 = (nt - 1 - nth) * BM;
+  const int off = s.lk - s.lq;
+  const int wr = row0 + (SPLIT ? (wave & 1) * 64 : wave * 32), d0 = SPLIT ? (wave >> 1) * ND : 0;
+  const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv), wq_last = div_by(min(wr + 32 * NJ, rows) - 1, a.g_inv) + off;
+  const int kend = max(0, a.causal ? min(s.lk, last_tok + off + 1) : s.lk);
+  const raw16* const K = (const raw16*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;
+  const raw16* const D = (const raw16*)b.dS + ((long)hk * a.total_k + s.kbeg) * b.ds_ld + row0;
+  f32x16 acc[NJ][ND];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int d = 0; d < ND; ++d) acc[j][d] = zero16();
+  PieceTile<bf16_t, DH, AL, KT, 256> tk;
+  // dS^T tile: 16 pieces of 8 rows per key
+  uint4 td[NP];
+  const int dk = tid / 16, dr = tid % 16 * 8;
+  auto load_d = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < NP; ++i) td[i] = *(const uint4*)(D + (long)min(k0 + dk + 16 * i, kend - 1) * b.ds_ld + dr);
+  };
+  if (kend > 0) {
+    tk.load(K, a.k_row, kend, dh, tid);
+    load_d(0);
+  }
+  for (int k0 = 0; k0 < kend; k0 += KT) {
+    // the first row written for this tile's keys, and the keys that exist
+    const int written = a.causal ? max(k0 / PACKED_KB * PACKED_KB - off, 0) * a.G / 32 * 32 : 0;
+    const bool keep = row0 + dr >= written && row0 + dr < (rows + 31) / 32 * 32;
+    __syncthreads();
+    tk.store(Ks, LD, kend - k0, dh, tid);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) *(uint4*)(Ds + (dk + 16 * i) * LDD + dr) = keep && k0 + dk + 16 * i < kend ? td[i] : make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    if (k0 + KT < kend) {
+      tk.load(K + (long)(k0 + KT) * a.k_row, a.k_row, kend - k0 - KT, dh, tid);
+      load_d(k0 + KT);
+    }
+    if (wr >= rows || (a.causal && k0 > wq_last)) continue;   // wave-uniform
+#pragma unroll
+    for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const int kr = kb * 32 + 16 * st + 4 * g;
+        bf16x8 bq[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) bq[j] = col_frag(Ds, LDD, kr, kr + 8, wr - row0 + j * 32, lane);
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const bf16x8 ka = col_frag(Ks, LD, kr, kr + 8, (d0 + d) * 32, lane);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[j][d] = mma32(ka, bq[j], acc[j][d]);
+        }
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int row = wr + j * 32 + r;
+    if (row >= rows) continue;
+    const int tok = div_by(row, a.g_inv), head = hk * a.G + row - tok * a.G;
+    store_row<bf16_t, AL, ND>((raw16*)b.dQ + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head + d0 * 32, acc[j], a.scale, g, dh - d0 * 32);
+  }
+}
+
 // dQ of 128 rows of one (sequence, kv head): 4 waves x 32 rows, whose Q and dO are registers; K and V tiles go through LDS.
 //   S^T[key][row] = K Q^T,  dP^T = V dO^T,  dQ^T[d][row] += K^T dS^T
 template <typename T, int DH, int AL>
@@ -154,9 +477,9 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
   raw *const Ks = kv, *const Vs = kv + KT * LD;
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
-  int seq, nth;
-  if (!find_slot(a.qoff, a.total_q, a.nseq, a.G, BM, slot, seq, nth)) return;
-  const SeqGeom s = seq_geom(a, seq);
+  int nth;
+  SeqGeom s;
+  if (!find_slot<false>(a, BM, slot, nth, s)) return;
   const int rows = s.lq * a.G, nt = (rows + BM - 1) / BM;
   if (nth >= nt) return;
   const int row0 = (nt - 1 - nth) * BM;
@@ -232,14 +555,24 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
 template <typename T, int DH, int AL>
 static void launch_bwd_al(const PackedAttnBwd& b, hipStream_t s) {
   const PackedAttn& a = b.f;
-  const dim3 gk((unsigned)(packed_slots(a.total_k, 128, a.nseq) * a.Hk));
-  const dim3 gq((unsigned)(packed_slots((long)a.total_q * a.G, PACKED_BM, a.nseq) * a.Hk));
+  const long kslots = packed_slots(a.total_k, PACKED_KB, a.nseq) * a.Hk, qslots = packed_slots((long)a.total_q * a.G, PACKED_BM, a.nseq) * a.Hk;
+  const dim3 gk((unsigned)kslots), gq((unsigned)qslots);
+  prof_mark(s, "attention.dkv");
   if constexpr (sizeof(T) == 4 && DH > 128) {
     packed_dkv_kernel<T, DH, AL, 1><<<gk, 256, 0, s>>>(b);
     packed_dkv_kernel<T, DH, AL, 2><<<gk, 256, 0, s>>>(b);
+  } else if constexpr (sizeof(T) == 2 && DH <= 128) {
+    packed_dkv_ws_kernel<DH, AL><<<dim3((unsigned)(kslots * b.rparts)), 512, 0, s>>>(b);
+    if (b.rparts > 1) packed_dkv_join_kernel<DH, AL><<<gk, 512, 0, s>>>(b);
+    if (b.dS && a.total_q > 0) {
+      prof_mark(s, "attention.dq");
+      packed_dq_ds_kernel<DH, AL><<<gq, 256, 0, s>>>(b);
+      return;
+    }
   } else {
     packed_dkv_kernel<T, DH, AL, 0><<<gk, 256, 0, s>>>(b);
   }
+  prof_mark(s, "attention.dq");
   packed_dq_kernel<T, DH, AL><<<gq, 256, 0, s>>>(b);
 }
 template <typename T, int DH>
@@ -250,18 +583,37 @@ static void launch_bwd(const PackedAttnBwd& b, int align, hipStream_t s) {
   }
   launch_bwd_al<T, DH, sizeof(T)>(b, s);
 }
+template <typename T, int LR>
+static void launch_delta(const PackedAttnBwd& b, int align, float* delta, hipStream_t s) {
+  const PackedAttn& a = b.f;
+  const dim3 grid((unsigned)(((long)a.total_q * a.H + 256 / LR - 1) / (256 / LR)));
+  if (align == 16) {
+    packed_delta_kernel<T, LR, 16><<<grid, 256, 0, s>>>(a, b.dO, delta);
+    return;
+  }
+  if constexpr (sizeof(T) == 2) {
+    if (align == 8) {
+      packed_delta_kernel<T, LR, 8><<<grid, 256, 0, s>>>(a, b.dO, delta);
+      return;
+    }
+  }
+  packed_delta_kernel<T, LR, sizeof(T)><<<grid, 256, 0, s>>>(a, b.dO, delta);
+}
 template <typename T>
 static void launch_bwd_t(const PackedAttnBwd& b, int align, float* delta, hipStream_t s) {
   const PackedAttn& a = b.f;
-  const int lr = a.dh <= 64 ? 16 : a.dh <= 128 ? 32 : 64;
-  const dim3 gd((unsigned)(((long)a.total_q * a.H + 256 / lr - 1) / (256 / lr)));
-  if (a.total_q == 0) {   // (keys without a query get zeros below)
-  } else if (lr == 16)
-    packed_delta_kernel<T, 16><<<gd, 256, 0, s>>>(a, b.dO, delta);
-  else if (lr == 32)
-    packed_delta_kernel<T, 32><<<gd, 256, 0, s>>>(a, b.dO, delta);
-  else
-    packed_delta_kernel<T, 64><<<gd, 256, 0, s>>>(a, b.dO, delta);
+  prof_mark(s, "attention.delta");
+  if (a.total_q > 0) {   // (keys without a query get zeros below)
+    constexpr int N = Elem<T>::PER;
+    if (a.dh <= 8 * N)
+      launch_delta<T, 8>(b, align, delta, s);
+    else if (a.dh <= 16 * N)
+      launch_delta<T, 16>(b, align, delta, s);
+    else if (a.dh <= 32 * N)
+      launch_delta<T, 32>(b, align, delta, s);
+    else if constexpr (sizeof(T) == 4)
+      launch_delta<T, 64>(b, align, delta, s);
+  }
   if (a.dh <= 64)
     launch_bwd<T, 64>(b, align, s);
   else if (a.dh <= 96)

@@ -53,9 +53,13 @@ __global__ __launch_bounds__(256, 1) void packed_few_kernel(PackedAttn a) {
 
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 15, g = lane >> 4, dh = a.dh;
-  int seq = slot, nth = 0;
-  if (a.chunk && !find_slot(a.koff, a.total_k, a.nseq, 1, a.chunk, slot, seq, nth)) return;
-  const SeqGeom s = seq_geom(a, seq);
+  int nth = 0;
+  SeqGeom s;
+  if (a.chunk) {
+    if (!find_slot<true>(a, a.chunk, slot, nth, s)) return;
+  } else {
+    s = seq_geom(a, slot);
+  }
   const int rows = s.lq * a.G;   // at most frows = max_q * G <= 16
   const int key0 = nth * a.chunk, kend = a.chunk ? min(s.lk, key0 + a.chunk) : s.lk;
   if (rows <= 0 || (a.chunk && key0 >= s.lk)) return;   // (unsplit, a sequence without keys still gets its zeros)

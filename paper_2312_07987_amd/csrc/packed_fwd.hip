@@ -30,9 +30,8 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(Pack
     s.kbeg = s.lk = 0;
     row0 = slot * BM;
   } else {
-    int seq, nth;
-    if (!find_slot(a.qoff, a.total_q, a.nseq, a.G, BM, slot, seq, nth)) return;
-    s = seq_geom(a, seq);
+    int nth;
+    if (!find_slot<false>(a, BM, slot, nth, s)) return;
     // the last tiles, which see most keys, first
     const int nt = (s.lq * a.G + BM - 1) / BM;
     if (nth >= nt) return;
@@ -195,8 +194,9 @@ void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s) 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Joining of the parts: lse = log sum exp lse_p, O = sum_p exp(lse_p - lse) o_p, in part order.  A wave per (token, head); LR lanes hold a
-// row in pieces of four, 64 / LR parts are read side by side.  Reads each part once: bytes.
+// Joining of the parts: lse = log sum exp lse_p, O = sum_p exp(lse_p - lse) o_p, in part order within each of the lane groups that read parts
+// side by side.  A wave per (token, head); LR lanes hold a row in pieces of four, 64 / LR parts are read at a time.  Reads each part once: bytes,
+// and in small calls the latency of offsets -> lse -> rows, so the parts' lse are read once, a lane each, and handed out by shuffles.
 // ---------------------------------------------------------------------------------------------------------------------------
 template <typename T, int LR>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
@@ -205,46 +205,55 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
   const int lane = threadIdx.x & 63;
   const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (id >= (long)a.total_q * a.H) return;   // wave-uniform
-  const int tokg = (int)(id / a.H), head = (int)(id % a.H), hk = head / a.G;
-  // the token's sequence: the last one that begins at or before it (tiles of one row, without the slots' + i: empty sequences share a begin)
+  const int tokg = (int)(id / a.H), head = (int)(id - (long)tokg * a.H), hk = head / a.G;
+  // the token's sequence: the last one that begins at or before it (empty sequences share a begin with the next)
   int lo = 0, n = a.nseq;
-  bool any = true;
-  do {
-    const int step = (n + 63) >> 6, i = lo + min(lane * step, n - 1);
-    const unsigned long long m = __ballot(lane * step < n && a.qoff[i] <= tokg);
-    any = m != 0;
-    const int k = any ? __popcll(m) - 1 : 0;
+  while (n > 64) {
+    const int step = (n + 63) >> 6;
+    const unsigned long long m = __ballot(lane * step < n && a.qoff[lo + min(lane * step, n - 1)] <= tokg);
+    if (!m) return;
+    const int k = __popcll(m) - 1;
     lo += k * step;
     n = min(step, n - k * step);
-  } while (any && n > 1);
-  if (!any) return;
-  const int seq = __builtin_amdgcn_readfirstlane(lo);
-  const SeqGeom s = seq_geom(a, seq);
-  const int tok = tokg - s.qbeg;
-  if (tok < 0 || tok >= s.lq) return;
+  }
+  const int i = lo + min(lane, n - 1);
+  const SeqGeom mine = seq_geom(a, i);
+  const int few = a.chunk ? first_slot(a.koff, a.total_k, 1, a.chunk, i) : i;
+  const unsigned long long m = __ballot(lane < n && a.qoff[i] <= tokg);
+  if (!m) return;
+  const int k = __builtin_amdgcn_readfirstlane(__popcll(m) - 1);
+  const int lq = __builtin_amdgcn_readlane(mine.lq, k), lk = __builtin_amdgcn_readlane(mine.lk, k), few0 = __builtin_amdgcn_readlane(few, k);
+  const int tok = tokg - __builtin_amdgcn_readlane(mine.qbeg, k);
+  if (tok < 0 || tok >= lq) return;
   const int row = tok * a.G + head - hk * a.G;
-  const int nfew = a.fo ? (a.chunk ? (s.lk + a.chunk - 1) / a.chunk : 1) : 0;
-  const int few0 = a.fo ? (a.chunk ? first_slot(a.koff, a.total_k, 1, a.chunk, seq) : seq) : 0;
-  const int nall = a.nparts + nfew;
+  const int nfew = a.fo ? (a.chunk ? (lk + a.chunk - 1) / a.chunk : 1) : 0, nall = a.nparts + nfew;
   const long rows = (long)a.total_q * a.H;
-  auto lse_of = [&](int p) {
-    return p < a.nparts ? a.pl[p * rows + id] : a.fl[((long)(few0 + p - a.nparts) * a.Hk + hk) * a.frows + row];
-  };
-  float mx = -INFINITY;
-  for (int p = lane; p < nall; p += 64) mx = fmaxf(mx, lse_of(p));
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
-  const float mb = mx == -INFINITY ? 0.f : mx;
-  float tot = 0.f;
+  float mx = -INFINITY, tot = 0.f;
   f32x4 acc = f32x4{};
-  const int c = lane % LR * 4, sub = lane / LR;
+  const int c = lane % LR * 4, sub = lane / LR, cc = min(c, a.dhp - 4);
+  for (int b = 0; b < nall; b += 64) {   // 64 parts at a time
+    const int p = b + lane;
+    const float lp = p >= nall ? -INFINITY : p < a.nparts ? a.pl[p * rows + id] : a.fl[((long)(few0 + p - a.nparts) * a.Hk + hk) * a.frows + row];
+    float mn = lp;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) mn = fmaxf(mn, __shfl_xor(mn, d, 64));
+    mn = fmaxf(mn, mx);
+    if (mn == -INFINITY) continue;
+    const float w = __builtin_amdgcn_exp2f((lp - mn) * 1.44269504088896340736f), alpha = __builtin_amdgcn_exp2f((mx - mn) * 1.44269504088896340736f);
+    mx = mn;
+    acc *= alpha;
+    tot *= alpha;
+    const int many = min(64, nall - b);
 #pragma unroll 4
-  for (int p = sub; p < nall; p += NP) {
-    const float lp = lse_of(p), w = __builtin_amdgcn_exp2f((lp - mb) * 1.44269504088896340736f);
-    tot += w;
-    if (lp == -INFINITY || c >= a.dhp) continue;   // (a part that saw nothing of the row is not written)
-    const float* o = p < a.nparts ? a.po + (p * rows + id) * a.dhp : a.fo + (((long)(few0 + p - a.nparts) * a.Hk + hk) * a.frows + row) * a.dhp;
-    acc += w * *(const f32x4*)(o + c);
+    for (int q = 0; q < many; q += NP) {
+      const int p = b + min(q + sub, many - 1);
+      const float wp = q + sub < many ? __shfl(w, q + sub, 64) : 0.f;
+      const float* o = p < a.nparts ? a.po + (p * rows + id) * a.dhp : a.fo + (((long)(few0 + p - a.nparts) * a.Hk + hk) * a.frows + row) * a.dhp;
+      const f32x4 v = *(const f32x4*)(o + cc);
+      tot += wp;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = wp > 0.f ? fmaf(wp, v[j], acc[j]) : acc[j];   // (a part that saw nothing of the row is not written)
+    }
   }
 #pragma unroll
   for (int d = LR; d < 64; d <<= 1) {
@@ -253,7 +262,7 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
     for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], d, 64);
   }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
-  if (lane == 0 && a.lse) a.lse[(long)head * a.total_q + tokg] = tot == 0.f ? -INFINITY : mb + log2f(tot) * 0.69314718055994530942f;
+  if (lane == 0 && a.lse) a.lse[(long)head * a.total_q + tokg] = tot == 0.f ? -INFINITY : mx + log2f(tot) * 0.69314718055994530942f;
   if (sub == 0) {
     raw* O = (raw*)a.O + (long)tokg * a.o_row + (long)head * a.o_head;
 #pragma unroll

@@ -204,21 +204,21 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormArgs a) {
   }
 }
 
-// dw[k][col] = the work-groups' partial sums, 16 strands of them in order, then the strands in order
+// dw[k][col] = the work-groups' partial sums, 32 strands of them in order, then the strands in order
 __global__ __launch_bounds__(256) void qk_norm_dw_kernel(const float* part, int blocks, int dh, float* dw0, float* dw1) {
-  __shared__ float s[16][17];
-  const int c = threadIdx.x & 15, q = threadIdx.x >> 4, i = blockIdx.x * 16 + c;
+  __shared__ float s[32][9];
+  const int c = threadIdx.x & 7, q = threadIdx.x >> 3, i = blockIdx.x * 8 + c;
   float x = 0.f;
   if (i < 2 * dh) {
 #pragma unroll 8
-    for (int b = q; b < blocks; b += 16) x += part[(long)b * 2 * dh + i];
+    for (int b = q; b < blocks; b += 32) x += part[(long)b * 2 * dh + i];
   }
   s[q][c] = x;
   __syncthreads();
   if (q == 0 && i < 2 * dh) {
     float t = 0.f;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) t += s[j][c];
+    for (int j = 0; j < 32; ++j) t += s[j][c];
     float* dw = i < dh ? dw0 : dw1;
     if (dw) dw[i % dh] = t;
   }
@@ -237,8 +237,8 @@ QkNormGrid qk_norm_grid(long tokens, int heads, int dh, int bf16) {
   const int per = 256 / row_lanes(dh, bf16);
   QkNormGrid g;
   const long blocks = (tokens + per - 1) / per;
-  g.x = (int)(blocks < 2048 ? blocks : 2048);
-  int parts = (int)(2048 / g.x);
+  g.x = (int)(blocks < 1024 ? blocks : 1024);
+  int parts = (int)(1024 / g.x);
   parts = parts < 1 ? 1 : parts > heads ? heads : parts;
   g.hchunk = (heads + parts - 1) / parts;
   g.y = (heads + g.hchunk - 1) / g.hchunk;
@@ -282,7 +282,7 @@ void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipSt
     else
       launch_norm_lr<float, 64>(a, align, grid, backward, s);
   }
-  if (backward && (a.dw[0] || a.dw[1])) qk_norm_dw_kernel<<<dim3((2 * a.dh + 15) / 16), 256, 0, s>>>(a.part, g.x * g.y, a.dh, a.dw[0], a.dw[1]);
+  if (backward && (a.dw[0] || a.dw[1])) qk_norm_dw_kernel<<<dim3((2 * a.dh + 7) / 8), 256, 0, s>>>(a.part, g.x * g.y, a.dh, a.dw[0], a.dw[1]);
 }
 
 }  // namespace sh
