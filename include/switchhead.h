@@ -282,8 +282,8 @@ typedef struct {
   int32_t nheads, nkv_heads, d_head;   /* nheads a multiple of nkv_heads; d_head <= 256                              */
   int32_t causal, dtype;
   int32_t total_q, total_k;            /* rows of Q and of K, V                                                      */
-  int32_t max_q;                       /* no sequence has more queries: further ones are treated as not there        */
-  int32_t max_k;                       /* about the most own keys of a sequence: chooses how work is split, no more   */
+  int32_t max_q, max_k;                /* no sequence has more queries, or own keys: further ones are treated as not
+                                          there.  They size the grids and choose how work is split                   */
   int32_t prefix;                      /* rows of K_prefix, V_prefix [prefix, nkv_heads, d_head] that every query sees
                                           in front of its own keys; 0: none                                          */
   float scale;                         /* > 0, or 0 for 1 / sqrt(d_head)                                             */

@@ -63,6 +63,7 @@ struct AttnPlan {
   int G, esz;
   bool few, two_parts;        // few rows per sequence: packed_few.hip; the prefix as a part of its own, for the rows of all sequences together
   int chunk, nsplit, nflat;   // keys of a few-row work-group (0: all); key ranges of the own keys and of the prefix
+  int groups, levels, levels128, klevels;   // wave groups of a tile's work-group; levels of the row tiles and of the key tiles, 0: by slot
   int dhp;
   size_t po, pl, fo, fl, total;
 };
@@ -87,6 +88,7 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   p.G = a.nheads / a.nkv_heads;
   p.esz = a.dtype == SH_BF16 ? 2 : 4;
   if (a.max_q > a.total_q) a.max_q = a.total_q;
+  if (a.max_k > a.total_k) a.max_k = a.total_k;
   if (!fill_strides(a.q_row, a.q_head, a.nheads, a.d_head) || !fill_strides(a.k_row, a.k_head, a.nkv_heads, a.d_head) ||
       !fill_strides(a.v_row, a.v_head, a.nkv_heads, a.d_head) || !fill_strides(a.o_row, a.o_head, a.nheads, a.d_head) ||
       !fill_strides(a.kp_row, a.kp_head, a.nkv_heads, a.d_head) || !fill_strides(a.vp_row, a.vp_head, a.nkv_heads, a.d_head))
@@ -101,6 +103,14 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   p.two_parts = false;
   p.chunk = 0;
   p.nsplit = p.nflat = 0;
+  p.groups = 1;
+  // levels where their grid is at most twice that of slots, or small
+  auto levels = [&](long most, long all, int tile) {
+    const long n = ceil_div(most, tile);
+    return a.causal && n * a.nseq <= 2 * packed_slots(all, tile, a.nseq) + 1024 / a.nkv_heads ? (int)n : 0;
+  };
+  p.levels = p.levels128 = levels(most, rows, PACKED_BM);
+  p.klevels = levels(a.max_k, a.total_k, PACKED_KB);
   const long seqs = a.nseq > 0 ? a.nseq : 1;
   // A prefix: sequences whose rows fill half a tile or more walk it themselves, ahead of their own keys; shorter ones put the rows of all
   // sequences into common tiles over the prefix, and their own keys are a second part.
@@ -117,10 +127,15 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
     if (a.max_k > 2 * chunk || (a.max_k > chunk && seqs * a.nkv_heads < 256)) p.chunk = (int)chunk;
   } else {
     // Few tiles and many keys: several work-groups share a tile's keys
-    const long tiles = (rows / PACKED_BM + (seqs + 1) / 2) * a.nkv_heads;
+    const long tiles = (rows / PACKED_BM + seqs) * a.nkv_heads;
     const long kts = ceil_div((long)(p.two_parts ? 0 : a.prefix) + a.max_k, kt);
-    long ns = tiles < 384 ? 512 / (tiles > 0 ? tiles : 1) : 1;
-    if (ns > kts / 4) ns = kts / 4;
+    p.groups = a.d_head <= 128 && kts >= 8 && tiles < 1024 ? 2 : 1;
+    if (p.esz == 2 && a.d_head <= 128 && most >= 1024 && ceil_div(rows, PACKED_BM2) * a.nkv_heads >= 256) {
+      p.groups = 4;
+      p.levels = levels(most, rows, PACKED_BM2);
+    }
+    long ns = 512 / p.groups / tiles;
+    if (ns > kts / 8) ns = kts / 8;
     if (ns > 32) ns = 32;
     p.nsplit = ns >= 2 || p.two_parts ? (int)(ns > 0 ? ns : 1) : 0;
   }
@@ -214,6 +229,7 @@ PackedAttn packed_args(const AttnPlan& p, const int32_t* qoff, const int32_t* ql
   a.causal = d.causal;
   a.prefix = d.prefix;
   a.max_q = d.max_q;
+  a.max_k = d.max_k;
   a.total_q = d.total_q;
   a.total_k = d.total_k;
   a.q_row = d.q_row;
@@ -230,6 +246,8 @@ PackedAttn packed_args(const AttnPlan& p, const int32_t* qoff, const int32_t* ql
   a.vp_head = d.vp_head;
   a.scale = d.scale;
   a.dhp = p.dhp;
+  a.groups = p.groups;
+  a.levels = p.levels;
   return a;
 }
 
@@ -329,6 +347,7 @@ sh_status switchhead_attention_forward(const sh_attention* d, const void* Q, con
     prof_mark(st, "attention.prefix");
     PackedAttn f = a;
     f.flat = 1;
+    f.groups = 1;
     f.nsplit = p.nflat;
     launch_packed_fwd(f, bf16, align, st);
   }
@@ -379,6 +398,7 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
   const int align = alignment({Q, K, V, O, dO, dQ, dK, dV}, {s.q_row, s.q_head, s.k_row, s.k_head, s.v_row, s.v_head, s.o_row, s.o_head}, s.d_head, p.esz);
   PackedAttnBwd b{};
   b.f = packed_args(p, q_offsets, q_lengths, k_offsets, k_lengths);
+  b.f.levels = p.levels128;
   b.f.Q = Q;
   b.f.K = K;
   b.f.V = V;
@@ -392,6 +412,8 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
   b.delta = delta;
   b.rchunk = w.rchunk;
   b.rparts = w.rparts;
+  b.kslots = packed_slots(s.total_k, PACKED_KB, s.nseq) * s.nkv_heads;
+  b.klevels = p.klevels;
   b.dkv = (float*)((char*)workspace + w.dkv);
   b.dkv_floats = w.dkv_floats;
   b.ds_ld = w.ds_ld;

@@ -10,6 +10,13 @@
 // one or more, a wave finds the slot's sequence with one probe per lane and round (64 sequences one round, 4096 two).  At most one
 // slot per sequence is empty.
 //
+// Levels.  Under a causal mask the tiles differ in length, and a launch that ends with a long one waits for it.  Where the longest sequence is not so
+// much longer than the others that the grid would be mostly empty, work-groups are numbered by the tile's distance from the light end of its sequence,
+// farthest first: (level, sequence) with as many levels as the longest sequence has tiles.  Tiles then start in falling order of length, and the
+// sequence needs no search.  Work-group ids are dealt to the eight XCDs in turn whatever their load, so a sequence's place within a level moves by one
+// from level to level (level_seq): with it standing still the longest sequence's tiles met on half of the XCDs (dK / dV of 16384 tokens 365 us
+// against 170 by slots).
+//
 // Operands.  32 x 32 products over 16 reduction indices: lane = 32 g + r holds A[row r][k = 8 g .. 8 g + 7] and B[k][column r], register q of
 // the result is D[8 (q / 4) + 4 g + q % 4][column r].  fp32 takes the same 8 values per lane through eight 32x32x2 instructions (the i-th
 // multiplies k = i and k = 8 + i), so both types share every index below.
@@ -23,7 +30,7 @@ struct PackedAttn {
   void* O;
   float* lse;                          // [H][total_q] or NULL
   const int *qoff, *qlen, *koff, *klen;   // qlen, klen may be NULL: the offsets' differences
-  int nseq, H, Hk, G, dh, causal, prefix, max_q;
+  int nseq, H, Hk, G, dh, causal, prefix, max_q, max_k;
   int total_q, total_k;
   long q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head, kp_row, kp_head, vp_row, vp_head;
   float scale;
@@ -31,6 +38,8 @@ struct PackedAttn {
   // Key ranges that other work-groups take as well leave normalised fp32 rows and their log-sum-exp (natural logarithm, -inf: nothing seen):
   // `dense` parts [part][total_q * H] and, from the few-row kernel, [slot * Hk + kv head][frows].
   int nsplit, part0;                   // this launch's parts of the keys, the first one's number; nsplit 0: O is written
+  int levels;                          // tiles of the longest sequence: work-groups numbered by level; 0: by slot
+  int groups;                          // 1, 2: wave groups of a work-group of 128 rows; 4: 256 rows (packed_fwd.hip)
   int flat, own;                       // flat: rows of all tokens over the prefix alone; own: the sequence's own keys alone
   float *po, *pl;
   int dhp;                             // part row length: dh rounded up to 4
@@ -51,8 +60,9 @@ struct PackedAttnBwd {
   // rows of a dK / dV work-group (a multiple of 32): key tiles that see more leave fp32 parts, [part][slot * Hk + kv head][dV, dK] of
   // dkv_floats each, for a second kernel
   int rchunk, rparts;
+  int klevels;                         // as levels, of the key tiles
   float* dkv;
-  long dkv_floats;
+  long dkv_floats, kslots;             // (slots * Hk)
 };
 
 struct SeqGeom {
@@ -69,6 +79,7 @@ __device__ __forceinline__ SeqGeom seq_geom(const PackedAttn& a, int i) {
   s.kbeg = clamp_to(a.koff[i], 0, a.total_k);
   s.lk = clamp_to(a.koff[i + 1], s.kbeg, a.total_k) - s.kbeg;
   if (a.klen) s.lk = clamp_to(a.klen[i], 0, s.lk);
+  s.lk = min(s.lk, a.max_k);
   return s;
 }
 __device__ __forceinline__ int first_slot(const int* off, int total, int mul, int tile, int i) {
@@ -103,6 +114,8 @@ __device__ __forceinline__ bool find_slot(const PackedAttn& a, int tile, int slo
   s.lk = __builtin_amdgcn_readlane(mine.lk, k);
   return true;
 }
+
+__device__ __forceinline__ int level_seq(int id, int nseq) { return (id % nseq + id / nseq) % nseq; }
 
 // ---- 16-byte pieces of rows -----------------------------------------------------------------------------------------------
 // AL: alignment in bytes of every row (16, 8, or the element): how a piece may be read and written.
@@ -164,34 +177,45 @@ __device__ __forceinline__ uint4 cut_piece(uint4 v, int d, int dh) {
 
 // NROWS rows on their way from memory to LDS.  load() carries no tests: a row past the last valid one repeats it and a column past dh
 // repeats column 0; store() puts zeros in both places (a key that no query sees has probability 0, and 0 times what lies behind a
-// sequence need not be 0).
+// sequence need not be 0).  The pieces' places within a tile are worked out once (place): a tile is a uniform base and 32-bit offsets.
 template <typename T, int DH, int AL, int NROWS, int NT>
 struct PieceTile {
   typedef typename Elem<T>::raw raw;
   static constexpr int PER = Elem<T>::PER, CPR = DH / PER, TOTAL = NROWS * CPR, NCH = (TOTAL + NT - 1) / NT;
   uint4 r[NCH];
+  unsigned ro[NCH];   // byte offset of the piece's row
+  __device__ __forceinline__ void place(long row_stride, int tid) {
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) ro[i] = (unsigned)min((tid + i * NT) / CPR, NROWS - 1) * (unsigned)row_stride * (unsigned)sizeof(raw);
+  }
   __device__ __forceinline__ void load(const raw* src, long row_stride, int valid, int dh, int tid) {
-    if (valid <= 0) return;   // uniform
-    const int last = min(valid, NROWS) - 1;
+    const unsigned last = (unsigned)(min(valid, NROWS) - 1) * (unsigned)row_stride * (unsigned)sizeof(raw);   // uniform
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int c = tid + i * NT;
-      r[i] = load_row_piece<T, AL>((const raw*)((const char*)src + (unsigned)min(c / CPR, last) * (unsigned)row_stride * (unsigned)sizeof(raw)), c % CPR * PER, dh);
+      const int d = (tid + i * NT) % CPR * PER;
+      const unsigned o = min(ro[i], last);
+      if constexpr (AL == 16)
+        r[i] = *(const uint4*)((const char*)src + (o + (unsigned)(d < dh ? d : 0) * (unsigned)sizeof(raw)));
+      else
+        r[i] = load_row_piece<T, AL>((const raw*)((const char*)src + o), d, dh);
     }
   }
   __device__ __forceinline__ void store(raw* t, int ld, int valid, int dh, int tid) const {
     const bool whole = valid >= NROWS && dh == DH;   // uniform
+    if (whole) {
+#pragma unroll
+      for (int i = 0; i < NCH; ++i) {
+        const int c = tid + i * NT;
+        if (TOTAL % NT == 0 || c < TOTAL) *(uint4*)(t + c / CPR * ld + c % CPR * PER) = r[i];
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int c = tid + i * NT;
-      if (TOTAL % NT != 0 && c >= TOTAL) continue;
-      const int row = c / CPR, d = c % CPR * PER;
-      uint4 v = r[i];
-      if (!whole) {
-        v = cut_piece<T, AL>(v, d, dh);
-        if (row >= valid) v = make_uint4(0, 0, 0, 0);
-      }
-      *(uint4*)(t + row * ld + d) = v;
+      const int c = tid + i * NT, row = c / CPR, d = c % CPR * PER;
+      uint4 v = cut_piece<T, AL>(r[i], d, dh);
+      const unsigned keep = row < valid ? 0xffffffffu : 0u;
+      if (TOTAL % NT == 0 || c < TOTAL) *(uint4*)(t + row * ld + d) = make_uint4(v.x & keep, v.y & keep, v.z & keep, v.w & keep);
     }
   }
 };
@@ -213,11 +237,20 @@ struct FragOf<float> {
 template <typename T>
 using frag_t = typename FragOf<T>::type;
 
-// LDS row stride: 16-byte fragment reads of 8 rows fall on all banks, and so do the rows that a transposing read (bf16) or the two lane
-// halves' column reads (fp32) touch at a time
+// LDS row strides in elements.  row_ld: rows 4 banks apart (of 64), the 16 rows that a fragment read touches at a time fall on all banks.  col_ld: rows 16
+// banks apart, so the 4 rows x 64 bytes that two groups of 16 lanes of a transposing read touch do (bf16); the two lane halves' rows 32 banks apart (fp32).
+// tile_ld: for tiles that are read both ways, twofold conflicts in either.
 template <typename T, int DH>
 constexpr int tile_ld() {
   return sizeof(T) == 2 ? DH + 16 : DH + 8;
+}
+template <typename T, int DH>
+constexpr int row_ld() {
+  return sizeof(T) == 2 ? DH + 8 : DH + 4;
+}
+template <typename T, int DH>
+constexpr int col_ld() {
+  return sizeof(T) == 4 ? DH + 8 : DH % 128 == 96 ? DH : DH / 128 * 128 + (DH % 128 ? 96 : 32);
 }
 
 __device__ __forceinline__ bf16x8 row_frag(const unsigned short* p) { return *(const bf16x8*)p; }
@@ -245,19 +278,27 @@ __device__ __forceinline__ f32x8 col_frag(const float* tile, int ld, int k0, int
   return f;
 }
 
-// elements d .. d + 7 of a row in memory, zeros from dh on; zeros altogether for a row that is not there
-template <typename T, int AL>
-__device__ __forceinline__ frag_t<T> mem_frag(const typename Elem<T>::raw* row, int d, int dh, bool valid) {
-  union {
+// The fragments d = 16 kk + 8 g (STEP 16) of a row in memory, zeros from dh on; zeros altogether for a row that is not there (the address must be
+// that of some row).  All loads are under way before the first is looked at: a test around each would make it a trip to memory of its own.
+template <typename T, int AL, int N, int STEP>
+__device__ __forceinline__ void mem_frags(frag_t<T>* f, const typename Elem<T>::raw* row, int d0, int dh, bool valid) {
+  union U {
     uint4 q[sizeof(T) / 2];
     frag_t<T> v;
-  } u;
+  } u[N];
 #pragma unroll
-  for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
-    u.q[j] = make_uint4(0, 0, 0, 0);
-    if (valid) u.q[j] = cut_piece<T, AL>(load_row_piece<T, AL>(row, d + j * Elem<T>::PER, dh), d + j * Elem<T>::PER, dh);
+  for (int kk = 0; kk < N; ++kk)
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) u[kk].q[j] = load_row_piece<T, AL>(row, kk * STEP + d0 + j * Elem<T>::PER, dh);
+#pragma unroll
+  for (int kk = 0; kk < N; ++kk) {
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) {
+      u[kk].q[j] = cut_piece<T, AL>(u[kk].q[j], kk * STEP + d0 + j * Elem<T>::PER, dh);
+      if (!valid) u[kk].q[j] = make_uint4(0, 0, 0, 0);
+    }
+    f[kk] = u[kk].v;
   }
-  return u.v;
 }
 
 __device__ __forceinline__ void pack_frag(bf16x8& o, const float* v) {
@@ -337,7 +378,7 @@ void launch_packed_few(const PackedAttn& a, int bf16, int align, hipStream_t s);
 void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s);
 void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta, hipStream_t s);
 
-enum { PACKED_BM = 128, PACKED_FEW = 16, PACKED_KB = 128 };
+enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128 };
 // head width that a work-group's tiles are laid out for
 static inline int packed_width(int dh) { return dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
 // slots of `rows` rows in tiles of bm over nseq sequences

@@ -7,6 +7,19 @@ namespace sh {
 
 typedef unsigned short raw16;
 
+// A work-group's 128 rows: those that see most keys first
+__device__ __forceinline__ bool row_tile(const PackedAttn& a, int id, int& row0, SeqGeom& s) {
+  if (a.levels) {
+    s = seq_geom(a, level_seq(id, a.nseq));
+    row0 = (a.levels - 1 - id / a.nseq) * PACKED_BM;
+    return row0 < s.lq * a.G;
+  }
+  int nth;
+  if (!find_slot<false>(a, PACKED_BM, id, nth, s)) return false;
+  row0 = ((s.lq * a.G + PACKED_BM - 1) / PACKED_BM - 1 - nth) * PACKED_BM;
+  return row0 >= 0;
+}
+
 // delta[head][token] = <dO, O>, from the rows as they are stored: LR lanes hold a row in 16-byte pieces.  (O's rounding is an error of
 // P delta that dS = P (dP - delta) shares with the plain form's rounded O; dS is rounded once more on its way into the products.)
 template <typename T, int LR, int AL>
@@ -59,11 +72,8 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
   {
     const raw* K = (const raw*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head;
     const raw* V = (const raw*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head;
-#pragma unroll
-    for (int kk = 0; kk < NKD; ++kk) {
-      kf[kk] = mem_frag<T, AL>(K, kk * 16 + 8 * g, dh, key < s.lk);
-      if constexpr (DK) vf[kk] = mem_frag<T, AL>(V, kk * 16 + 8 * g, dh, key < s.lk);
-    }
+    mem_frags<T, AL, NKD, 16>(kf, K, 8 * g, dh, key < s.lk);
+    if constexpr (DK) mem_frags<T, AL, NKD, 16>(vf, V, 8 * g, dh, key < s.lk);
   }
   f32x16 accK[DK ? NDB : 1], accV[DV ? NDB : 1];
 #pragma unroll
@@ -154,6 +164,20 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
   }
 }
 
+// A work-group's key tile: its number in the sequence, and the slot that its parts go to.  By level: the first tiles, which most rows see, first.
+__device__ __forceinline__ bool key_tile(const PackedAttnBwd& b, int id, int& nth, int& slot, SeqGeom& s) {
+  const PackedAttn& a = b.f;
+  if (!b.klevels) {
+    slot = id;
+    return find_slot<true>(a, PACKED_KB, id, nth, s);
+  }
+  const int seq = level_seq(id, a.nseq);
+  s = seq_geom(a, seq);
+  nth = (s.lk + PACKED_KB - 1) / PACKED_KB - b.klevels + id / a.nseq;
+  slot = first_slot(a.koff, a.total_k, 1, PACKED_KB, seq) + nth;
+  return nth >= 0;
+}
+
 // The same for bf16 heads of 33 .. 128 elements with two kinds of waves.  A single wave per SIMD, which is all that the kernel above has registers
 // for, leaves the matrix cores idle during exponentials, conversions and LDS traffic.  Here waves 0 .. 3 (score) hold the K and V fragments
 // of 32 keys each, form P and dS of a tile of 32 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
@@ -174,11 +198,11 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
   int bid = blockIdx.x;
   const int hk = bid % a.Hk;
   bid /= a.Hk;
-  const int part = bid % b.rparts, slot = bid / b.rparts;
+  const int nslot = gridDim.x / (a.Hk * b.rparts), part = bid / nslot, slot_ = bid % nslot;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, blk = wave & 3, r = lane & 31, g = lane >> 5, dh = a.dh;
-  int nth;
+  int nth, slot;
   SeqGeom s;
-  if (!find_slot<true>(a, KB, slot, nth, s)) return;
+  if (!key_tile(b, slot_, nth, slot, s)) return;
   const int k0 = nth * KB;
   if (k0 >= s.lk) return;
   const int off = s.lk - s.lq, rows = s.lq * a.G, key = k0 + blk * 32 + r, wk_first = k0 + blk * 32;
@@ -193,11 +217,8 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
     bf16x8 kf[NKD], vf[NKD];
     const unsigned short* K = (const unsigned short*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head;
     const unsigned short* V = (const unsigned short*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head;
-#pragma unroll
-    for (int kk = 0; kk < NKD; ++kk) {
-      kf[kk] = mem_frag<bf16_t, AL>(K, kk * 16 + 8 * g, dh, key < s.lk);
-      vf[kk] = mem_frag<bf16_t, AL>(V, kk * 16 + 8 * g, dh, key < s.lk);
-    }
+    mem_frags<bf16_t, AL, NKD, 16>(kf, K, 8 * g, dh, key < s.lk);
+    mem_frags<bf16_t, AL, NKD, 16>(vf, V, 8 * g, dh, key < s.lk);
     // (keys past the sequence have no row of dS^T: they repeat the last key's address and do not store)
     unsigned short* dsrow = nullptr;
     if (b.dS) dsrow = (unsigned short*)b.dS + ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 4 * g;
@@ -339,7 +360,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
     return;
   }
   // a part: accumulators in register order, 16 bytes per lane
-  f32x4* out = (f32x4*)(b.dkv + ((long)part * gridDim.x / b.rparts + (long)slot * a.Hk + hk) * b.dkv_floats) + blk * NDB * 4 * 64 + lane;
+  f32x4* out = (f32x4*)(b.dkv + ((long)part * b.kslots + (long)slot * a.Hk + hk) * b.dkv_floats) + blk * NDB * 4 * 64 + lane;
 #pragma unroll
   for (int d = 0; d < NDB; ++d)
 #pragma unroll
@@ -368,7 +389,7 @@ __global__ __launch_bounds__(512) void packed_dkv_join_kernel(PackedAttnBwd b) {
 #pragma unroll
   for (int d = 0; d < NDB; ++d) acc[d] = zero16();
   for (int p = p0; p <= p1; ++p) {
-    const f32x4* in = (const f32x4*)(b.dkv + ((long)p * gridDim.x + (long)slot * a.Hk + hk) * b.dkv_floats) + ((wave >= 4 ? 4 : 0) + blk) * NDB * 4 * 64 + lane;
+    const f32x4* in = (const f32x4*)(b.dkv + ((long)p * b.kslots + (long)slot * a.Hk + hk) * b.dkv_floats) + ((wave >= 4 ? 4 : 0) + blk) * NDB * 4 * 64 + lane;
 #pragma unroll
     for (int d = 0; d < NDB; ++d)
 #pragma unroll
@@ -392,18 +413,16 @@ __global__ __launch_bounds__(512) void packed_dkv_join_kernel(PackedAttnBwd b) {
 template <int DH, int AL>
 __global__ __launch_bounds__(256, 2) void packed_dq_ds_kernel(PackedAttnBwd b) {
   const PackedAttn& a = b.f;
-  constexpr int KT = 64, LD = DH + 16, BM = PACKED_BM, LDD = BM + 16, NDB = DH / 32, NP = KT * BM / 8 / 256;
+  constexpr int KT = 64, LD = col_ld<bf16_t, DH>(), BM = PACKED_BM, LDD = col_ld<bf16_t, BM>(), NDB = DH / 32, NP = KT * BM / 8 / 256;
   constexpr bool SPLIT = NDB % 2 == 0;
   constexpr int NJ = SPLIT ? 2 : 1, ND = SPLIT ? NDB / 2 : NDB;
   __shared__ __attribute__((aligned(16))) unsigned short Ks[KT * LD], Ds[KT * LDD];
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
-  int nth;
   SeqGeom s;
-  if (!find_slot<false>(a, BM, slot, nth, s)) return;
-  const int rows = s.lq * a.G, nt = (rows + BM - 1) / BM;
-  if (nth >= nt) return;
-  const int row0 = (nt - 1 - nth) * BM;
+  int row0;
+  if (!row_tile(a, slot, row0, s)) return;
+  const int rows = s.lq * a.G;
   const int off = s.lk - s.lq;
   const int wr = row0 + (SPLIT ? (wave & 1) * 64 : wave * 32), d0 = SPLIT ? (wave >> 1) * ND : 0;
   const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv), wq_last = div_by(min(wr + 32 * NJ, rows) - 1, a.g_inv) + off;
@@ -423,6 +442,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_ds_kernel(PackedAttnBwd b) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) td[i] = *(const uint4*)(D + (long)min(k0 + dk + 16 * i, kend - 1) * b.ds_ld + dr);
   };
+  tk.place(a.k_row, tid);
   if (kend > 0) {
     tk.load(K, a.k_row, kend, dh, tid);
     load_d(0);
@@ -477,12 +497,10 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
   raw *const Ks = kv, *const Vs = kv + KT * LD;
   const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
-  int nth;
   SeqGeom s;
-  if (!find_slot<false>(a, BM, slot, nth, s)) return;
-  const int rows = s.lq * a.G, nt = (rows + BM - 1) / BM;
-  if (nth >= nt) return;
-  const int row0 = (nt - 1 - nth) * BM;
+  int row0;
+  if (!row_tile(a, slot, row0, s)) return;
+  const int rows = s.lq * a.G;
   const int off = s.lk - s.lq, row = row0 + wave * 32 + r;
   const int tok = div_by(min(row, rows - 1), a.g_inv), head = hk * a.G + min(row, rows - 1) - tok * a.G;
   const int qpos = tok + off;
@@ -494,11 +512,8 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
   frag_t<T> qf[NKD], gf[NKD];
   const raw* Q = (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head;
   const raw* G = (const raw*)b.dO + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head;
-#pragma unroll
-  for (int kk = 0; kk < NKD; ++kk) {
-    qf[kk] = mem_frag<T, AL>(Q, kk * 16 + 8 * g, dh, row < rows);
-    gf[kk] = mem_frag<T, AL>(G, kk * 16 + 8 * g, dh, row < rows);
-  }
+  mem_frags<T, AL, NKD, 16>(qf, Q, 8 * g, dh, row < rows);
+  mem_frags<T, AL, NKD, 16>(gf, G, 8 * g, dh, row < rows);
   const float lse2 = a.lse[(long)head * a.total_q + s.qbeg + tok] * 1.44269504088896340736f;
   const float del = b.delta[(long)head * a.total_q + s.qbeg + tok];
   f32x16 acc[NDB];
@@ -508,6 +523,8 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
   const raw* const K = (const raw*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;
   const raw* const V = (const raw*)a.V + (long)s.kbeg * a.v_row + (long)hk * a.v_head;
   PieceTile<T, DH, AL, KT, 256> tk, tv;
+  tk.place(a.k_row, tid);
+  tv.place(a.v_row, tid);
   if (kend > 0) {
     tk.load(K, a.k_row, kend, dh, tid);
     tv.load(V, a.v_row, kend, dh, tid);
@@ -556,13 +573,13 @@ template <typename T, int DH, int AL>
 static void launch_bwd_al(const PackedAttnBwd& b, hipStream_t s) {
   const PackedAttn& a = b.f;
   const long kslots = packed_slots(a.total_k, PACKED_KB, a.nseq) * a.Hk, qslots = packed_slots((long)a.total_q * a.G, PACKED_BM, a.nseq) * a.Hk;
-  const dim3 gk((unsigned)kslots), gq((unsigned)qslots);
+  const dim3 gk((unsigned)kslots), gq((unsigned)(a.levels ? (long)a.levels * a.nseq * a.Hk : qslots));
   prof_mark(s, "attention.dkv");
   if constexpr (sizeof(T) == 4 && DH > 128) {
     packed_dkv_kernel<T, DH, AL, 1><<<gk, 256, 0, s>>>(b);
     packed_dkv_kernel<T, DH, AL, 2><<<gk, 256, 0, s>>>(b);
   } else if constexpr (sizeof(T) == 2 && DH <= 128) {
-    packed_dkv_ws_kernel<DH, AL><<<dim3((unsigned)(kslots * b.rparts)), 512, 0, s>>>(b);
+    packed_dkv_ws_kernel<DH, AL><<<dim3((unsigned)((b.klevels ? (long)b.klevels * a.nseq * a.Hk : kslots) * b.rparts)), 512, 0, s>>>(b);
     if (b.rparts > 1) packed_dkv_join_kernel<DH, AL><<<gk, 512, 0, s>>>(b);
     if (b.dS && a.total_q > 0) {
       prof_mark(s, "attention.dq");

@@ -69,11 +69,6 @@ __global__ __launch_bounds__(256, 1) void packed_few_kernel(PackedAttn a) {
   const raw* const V = (const raw*)a.V + (long)s.kbeg * a.v_row + (long)hk * a.v_head;
   raw* const vl = fsm + wave * KP * LDV;
 
-  frag_t<T> qf[NK];
-  const raw* Q = (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head;
-#pragma unroll
-  for (int kk = 0; kk < NK; ++kk) qf[kk] = mem_frag<T, AL>(Q, kk * 32 + 8 * g, dh, r < rows);
-
   union KF {
     uint4 q[FP];
     frag_t<T> f;
@@ -95,13 +90,15 @@ __global__ __launch_bounds__(256, 1) void packed_few_kernel(PackedAttn a) {
       vf[i] = load_row_piece<T, AL>(V + (long)min(k0 + c / CPR, kend - 1) * a.v_row, c % CPR * PER, dh);
     }
   };
+  if (key0 + wave * KP < kend) load(key0 + wave * KP);
+  frag_t<T> qf[NK];
+  mem_frags<T, AL, NK, 32>(qf, (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head, 8 * g, dh, r < rows);
   f32x4 o[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d) o[d] = f32x4{};
   float m = -INFINITY, l = 0.f;
   const float sc = a.scale * 1.44269504088896340736f;
   const bool cut = dh != DH;
-  if (key0 + wave * KP < kend) load(key0 + wave * KP);
   for (int k0 = key0 + wave * KP; k0 < kend; k0 += W * KP) {
     f32x4 sv[2];
 #pragma unroll

@@ -4,23 +4,32 @@
 // Transposed products, S^T[key][row] = K Q^T and O^T[d][row] += V^T P^T: a row (token, head) is a lane column, so the running maximum
 // and sum of its softmax are lane-local up to one exchange between the lane halves, and exp(S^T) is the second product's operand as it
 // stands.  K and V tiles go through LDS once for all rows of the work-group.
+#include <type_traits>
+
 #include "packed_attn.h"
 
 namespace sh {
 
-// One work-group: 4 waves x 32 rows of one (sequence, kv head), key tiles of KT.
-template <typename T, int DH, int AL>
-__global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(PackedAttn a) {
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// One work-group: 128 rows of one (sequence, kv head), four waves of 32, key tiles of KT.  NG = 2: two such groups of waves take
+// alternate tiles of the same rows and merge their (o, m, l) through LDS at the end.  That halves the chain of a long row of tiles, which is what a
+// batch of few long and many short sequences waits for, and the group has the CU to itself, so its two buffers per group (one barrier per trip)
+// fit.  16384 packed tokens, longest 4096, 4 heads of 128: 127 us with one group, see the launch for what it is with two.
+template <typename T, int DH, int AL, int NG>
+__global__ __launch_bounds__(256 * NG, DH <= 128 && NG == 1 ? 2 : 1) void packed_fwd_kernel(PackedAttn a) {
   typedef typename Elem<T>::raw raw;
-  constexpr int KT = DH * sizeof(T) > 256 ? 32 : 64, LD = tile_ld<T, DH>(), NKD = DH / 16, NDB = DH / 32, BM = PACKED_BM;
-  __shared__ __attribute__((aligned(16))) raw kv[2 * KT * LD];
-  raw *const Ks = kv, *const Vs = kv + KT * LD;
+  constexpr int KT = DH * sizeof(T) > 256 ? 32 : 64, LDK = row_ld<T, DH>(), LDV = col_ld<T, DH>(), NKD = DH / 16, NDB = DH / 32, BM = PACKED_BM;
+  constexpr int NBUF = NG, TILE = KT * (LDK + LDV);
+  __shared__ __attribute__((aligned(16))) raw kv_[NG * NBUF * TILE];
 
   int b = blockIdx.x;
   const int hk = b % a.Hk;
   b /= a.Hk;
   const int ns = max(a.nsplit, 1), split = b % ns, slot = b / ns;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
+  const int grp = NG > 1 ? threadIdx.x >> 8 : 0;
+  const int tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
+  raw* const kv = kv_ + grp * NBUF * TILE;
 
   SeqGeom s;
   int row0;
@@ -29,6 +38,9 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(Pack
     s.lq = a.total_q;
     s.kbeg = s.lk = 0;
     row0 = slot * BM;
+  } else if (a.levels) {
+    s = seq_geom(a, level_seq(slot, a.nseq));
+    row0 = (a.levels - 1 - slot / a.nseq) * BM;
   } else {
     int nth;
     if (!find_slot<false>(a, BM, slot, nth, s)) return;
@@ -51,8 +63,7 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(Pack
 
   frag_t<T> qf[NKD];
   const raw* Q = (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head;
-#pragma unroll
-  for (int kk = 0; kk < NKD; ++kk) qf[kk] = mem_frag<T, AL>(Q, kk * 16 + 8 * g, dh, row < rows);
+  mem_frags<T, AL, NKD, 16>(qf, Q, 8 * g, dh, row < rows);
 
   f32x16 o[NDB];
 #pragma unroll
@@ -62,14 +73,21 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(Pack
 
   // tiles of the prefix, then of the own keys; this work-group's even share of them
   const int np = (prefix + KT - 1) / KT, nt = np + (kend + KT - 1) / KT;
-  const int t0 = (int)((long)nt * split / ns), t1 = (int)((long)nt * (split + 1) / ns);
+  const int t0 = (int)((unsigned)(nt * split) / (unsigned)ns), t1 = (int)((unsigned)(nt * (split + 1)) / (unsigned)ns);   // (below 2^25 tiles, 32 parts)
   PieceTile<T, DH, AL, KT, 256> tk, tv;
   const raw* const KP = (const raw*)a.KP + (long)hk * a.kp_head;
   const raw* const VP = (const raw*)a.VP + (long)hk * a.vp_head;
   const raw* const K = (const raw*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;
   const raw* const V = (const raw*)a.V + (long)s.kbeg * a.v_row + (long)hk * a.v_head;
   auto valid_of = [&](int t) { return t < np ? prefix - t * KT : kend - (t - np) * KT; };
+  // (the prefix may have other strides: the pieces are placed again at the border)
+  tk.place(t0 + grp < np ? a.kp_row : a.k_row, tid);
+  tv.place(t0 + grp < np ? a.vp_row : a.v_row, tid);
   auto load = [&](int t) {
+    if (t >= np && t < np + NG) {
+      tk.place(a.k_row, tid);
+      tv.place(a.v_row, tid);
+    }
     if (t < np) {
       tk.load(KP + (long)t * KT * a.kp_row, a.kp_row, valid_of(t), dh, tid);
       tv.load(VP + (long)t * KT * a.vp_row, a.vp_row, valid_of(t), dh, tid);
@@ -78,73 +96,115 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(Pack
       tv.load(V + (long)(t - np) * KT * a.v_row, a.v_row, valid_of(t), dh, tid);
     }
   };
-  if (t0 < t1) load(t0);
+  auto store = [&](int t, raw* buf) {
+    tk.store(buf, LDK, valid_of(t), dh, tid);
+    tv.store(buf + KT * LDK, LDV, valid_of(t), dh, tid);
+  };
+  if (t0 + grp < t1) load(t0 + grp);
   __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): what was loaded before the loop is not waited for again inside it
-  for (int t = t0; t < t1; ++t) {
-    const int valid = valid_of(t), k0 = (t - np) * KT;
+  if constexpr (NG == 2) {
+    if (t0 + grp < t1) store(t0 + grp, kv);
+    if (t0 + grp + 2 < t1) load(t0 + grp + 2);
     __syncthreads();
-    tk.store(Ks, LD, valid, dh, tid);
-    tv.store(Vs, LD, valid, dh, tid);
-    __syncthreads();
-    if (t + 1 < t1) load(t + 1);
-    const bool masked = a.causal && t >= np;
-    if (row0 + wave * 32 >= rows || (masked && k0 > wq_last)) continue;   // wave-uniform: no rows, or nothing that they see
-
-    float sv[KT / 32][16];
-#pragma unroll
-    for (int kb = 0; kb < KT / 32; ++kb) {
-      f32x16 acc = zero16();
-#pragma unroll
-      for (int kk = 0; kk < NKD; ++kk) acc = mma32(row_frag(&Ks[(kb * 32 + r) * LD + kk * 16 + 8 * g]), qf[kk], acc);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sv[kb][i] = acc[i];
+  }
+  // NG = 2, one barrier per trip: while a tile is multiplied out of one buffer the next one (requested a trip ago) is written into the other and
+  // the one after that starts to travel.  NG = 1: the tile in the registers is written between two barriers.  All waves make the same trips.
+  int cur = 0;
+  for (int tb = t0; tb < t1; tb += NG, cur ^= NBUF - 1) {
+    const int t = tb + grp, valid = valid_of(t), k0 = (t - np) * KT;
+    const raw *const Ks = kv + cur * TILE, *const Vs = Ks + KT * LDK;
+    if constexpr (NG == 2) {
+      if (t + 2 < t1) {
+        store(t + 2, kv + (cur ^ 1) * TILE);
+        if (t + 4 < t1) load(t + 4);
+      }
+    } else {
+      __syncthreads();
+      store(t, kv);
+      __syncthreads();
+      if (t + 1 < t1) load(t + 1);
     }
-    if (valid < KT || (masked && k0 + KT - 1 > wq_first)) {
-      const int lim = (masked ? min(valid - 1, qpos - k0) : valid - 1) - 4 * g;
+    const bool masked = a.causal && t >= np;
+    // wave-uniform: a tile past the end, no rows, or nothing that they see
+    if (t < t1 && row0 + wave * 32 < rows && !(masked && k0 > wq_last)) {
+      f32x16 sv[KT / 32];
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb) {
+        sv[kb] = zero16();
+#pragma unroll
+        for (int kk = 0; kk < NKD; ++kk) sv[kb] = mma32(row_frag(&Ks[(kb * 32 + r) * LDK + kk * 16 + 8 * g]), qf[kk], sv[kb]);
+      }
+      if (valid < KT || (masked && k0 + KT - 1 > wq_first)) {
+        const int lim = (masked ? min(valid - 1, qpos - k0) : valid - 1) - 4 * g;
+#pragma unroll
+        for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (kb * 32 + 8 * (i >> 2) + (i & 3) > lim) sv[kb][i] = -INFINITY;
+      }
+      float mt = -INFINITY;
 #pragma unroll
       for (int kb = 0; kb < KT / 32; ++kb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (kb * 32 + 8 * (i >> 2) + (i & 3) > lim) sv[kb][i] = -INFINITY;
-    }
-    float mt = -INFINITY;
+        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sv[kb][i]);
+      mt = fmaxf(mt, __shfl_xor(mt, 32, 64)) * sc;   // sc > 0
+      const float mn = fmaxf(m, mt);
+      if (__ballot(mn > m)) {   // most tiles move no maximum
+        const float alpha = mn > m ? __builtin_amdgcn_exp2f(m - mn) : 1.f;   // m = -inf: 0
+        l *= alpha;
 #pragma unroll
-    for (int kb = 0; kb < KT / 32; ++kb)
+        for (int d = 0; d < NDB; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sv[kb][i]);
-    mt = fmaxf(mt, __shfl_xor(mt, 32, 64)) * sc;   // sc > 0
-    const float mn = fmaxf(m, mt);
-    const bool moved = mn > m;
-    const float alpha = moved ? __builtin_amdgcn_exp2f(m - mn) : 1.f;   // m = -inf: 0
-    m = mn;
-    const float mb = mn == -INFINITY ? 0.f : mn;   // (a row that has seen no key yet)
-    float ps = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sv[kb][i] = __builtin_amdgcn_exp2f(fmaf(sv[kb][i], sc, -mb));   // masked: 0
-        ps += sv[kb][i];
+          for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
       }
-    l = l * alpha + ps;
-    if (__ballot(moved)) {
+      m = mn;
+      const float mb = mn == -INFINITY ? 0.f : mn;   // (a row that has seen no key yet)
+      float ps = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < KT / 32; ++kb)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          float p8[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            p8[i] = __builtin_amdgcn_exp2f(fmaf(sv[kb][8 * st + i], sc, -mb));   // masked: 0
+            ps += p8[i];
+          }
+          // P is rounded to the storage type for its product; the sum keeps 32 bits
+          frag_t<T> pb;
+          pack_frag(pb, p8);
+          const int kr = kb * 32 + 16 * st + 4 * g;
+#pragma unroll
+          for (int d = 0; d < NDB; ++d) o[d] = mma32(col_frag(Vs, LDV, kr, kr + 8, d * 32, lane), pb, o[d]);
+        }
+      l += ps;
+    }
+    if constexpr (NG == 2) __syncthreads();
+  }
+  l += __shfl_xor(l, 32, 64);
+  if constexpr (NG == 2) {
+    // group 1 parks its partial results over the tiles; group 0 of the same wave and lane holds the same row and elements
+    static_assert(4 * (NDB * 16 + 2) * 64 * 4 <= NG * NBUF * TILE * (int)sizeof(raw), "the parked accumulators fit over the tiles");
+    float* park = (float*)kv_ + wave * (NDB * 16 + 2) * 64 + lane;
+    if (grp == 1) {
 #pragma unroll
       for (int d = 0; d < NDB; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+        for (int i = 0; i < 16; ++i) park[(d * 16 + i) * 64] = o[d][i];
+      park[NDB * 16 * 64] = m;
+      park[(NDB * 16 + 1) * 64] = l;
     }
+    __syncthreads();
+    if (grp == 1) return;
+    const float m1 = park[NDB * 16 * 64], l1 = park[(NDB * 16 + 1) * 64], mn = fmaxf(m, m1), mb = mn == -INFINITY ? 0.f : mn;
+    const float f0 = __builtin_amdgcn_exp2f(m - mb), f1 = __builtin_amdgcn_exp2f(m1 - mb);   // a group that saw no key: 0
 #pragma unroll
-    for (int kb = 0; kb < KT / 32; ++kb)
+    for (int d = 0; d < NDB; ++d)
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        frag_t<T> pb;
-        pack_frag(pb, &sv[kb][8 * st]);
-        const int kr = kb * 32 + 16 * st + 4 * g;
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) o[d] = mma32(col_frag(Vs, LD, kr, kr + 8, d * 32, lane), pb, o[d]);
-      }
+      for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f0 + park[(d * 16 + i) * 64] * f1;
+    l = l * f0 + l1 * f1;
+    m = mn;
   }
-  l += __shfl_xor(l, 32, 64);
   if (row >= rows) return;
   const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // nothing seen: zeros; NaN stays
   const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
@@ -158,19 +218,301 @@ __global__ __launch_bounds__(256, DH <= 128 ? 2 : 1) void packed_fwd_kernel(Pack
   }
 }
 
-template <typename T, int DH>
-static void launch_fwd(const PackedAttn& a, int align, dim3 grid, hipStream_t s) {
-  if (align == 16) {
-    packed_fwd_kernel<T, DH, 16><<<grid, 256, 0, s>>>(a);
-    return;
+// the larger of the two lane halves' values, in both
+__device__ __forceinline__ float half_max(float x) {
+  const auto v = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
+}
+// ---------------------------------------------------------------------------------------------------------------------------
+// The same for bf16 and long rows of tiles: 4 waves x 64 rows, one wave per SIMD with all of its registers.
+//
+// What bounds the kernel above is that its waves read every K and V fragment for 32 rows only (the LDS pipe is then as busy as the matrix cores)
+// and do one thing at a time: products, then the softmax, then products, with LDS latency in front of each.  Here a fragment serves 64 rows, and the
+// loop is a pipeline over steps of 32 keys whose three parts do not depend on each other: in step s the products S(s + 1) = K Q^T, the softmax of S(s)
+// and the products O += V^T P(s - 1)^T, 32 matrix instructions (1024 cycles) beside the vector instructions of 32 exponentials a lane (about
+// 800), interleaved by the scheduling groups.  K and V tiles of 64 keys lie in three LDS stages each: one barrier per tile.
+// The running maximum moves only where a tile's exceeds it by more than 2^8 in the exponent's base (P then stays below 2^8, which costs bf16
+// nothing), so the accumulators are hardly ever scaled.
+// ---------------------------------------------------------------------------------------------------------------------------
+template <int DH, int AL, int NJ, int NW>
+__global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn a) {
+  typedef unsigned short raw;
+  constexpr int KT = 64, LDK = row_ld<bf16_t, DH>(), LDV = col_ld<bf16_t, DH>(), NKD = DH / 16, NDB = DH / 32, BM = NW * 32 * NJ, NT = 64 * NW, TK = KT * LDK, TV = KT * LDV;
+  constexpr bool ACC = NW == 4;   // one wave per SIMD: 256 more registers that only matrix instructions and moves reach
+  __shared__ __attribute__((aligned(16))) raw Ks[3 * TK], Vs[3 * TV];
+  int b = blockIdx.x;
+  const int hk = b % a.Hk;
+  b /= a.Hk;
+  const int ns = max(a.nsplit, 1), split = b % ns, slot = b / ns;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
+  SeqGeom s;
+  int row0;
+  if (a.levels) {
+    s = seq_geom(a, level_seq(slot, a.nseq));
+    row0 = (a.levels - 1 - slot / a.nseq) * BM;
+  } else {
+    int nth;
+    if (!find_slot<false>(a, BM, slot, nth, s)) return;
+    row0 = ((s.lq * a.G + BM - 1) / BM - 1 - nth) * BM;
   }
-  if constexpr (sizeof(T) == 2) {
-    if (align == 8) {
-      packed_fwd_kernel<T, DH, 8><<<grid, 256, 0, s>>>(a);
+  const int rows = s.lq * a.G;
+  if (row0 < 0 || row0 >= rows) return;
+  const int off = s.lk - s.lq, wr = row0 + wave * 32 * NJ;
+  const int wq_first = div_by(min(wr, rows - 1), a.g_inv) + off, wq_last = div_by(min(wr + 32 * NJ - 1, rows - 1), a.g_inv) + off;
+  const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv);
+  const int prefix = a.own ? 0 : a.prefix;
+  const int kend = max(0, a.causal ? min(s.lk, last_tok + off + 1) : s.lk);
+  int tok[NJ], head[NJ];
+  bf16x8 qf[NJ][NKD];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int row = min(wr + j * 32 + r, rows - 1);
+    tok[j] = div_by(row, a.g_inv);
+    head[j] = hk * a.G + row - tok[j] * a.G;
+    mem_frags<bf16_t, AL, NKD, 16>(qf[j], (const raw*)a.Q + (long)(s.qbeg + tok[j]) * a.q_row + (long)head[j] * a.q_head, 8 * g, dh, wr + j * 32 + r < rows);
+  }
+  f32x16 o[NJ][NDB];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int d = 0; d < NDB; ++d) o[j][d] = zero16();
+  float m[NJ], l[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    m[j] = -INFINITY;
+    l[j] = 0.f;
+  }
+  const float sc = a.scale * 1.44269504088896340736f;
+
+  const int np = (prefix + KT - 1) / KT, nt = np + (kend + KT - 1) / KT;
+  const int t0 = (int)((unsigned)(nt * split) / (unsigned)ns), t1 = (int)((unsigned)(nt * (split + 1)) / (unsigned)ns);
+  // this wave's tiles: up to the last one with a key that one of its rows sees
+  const int seen = !a.causal ? nt : np + (wq_last >= 0 ? wq_last / KT + 1 : 0);
+  const int tend = wr < rows ? min(t1, seen) : 0;
+  PieceTile<bf16_t, DH, AL, KT, NT> tk, tv;
+  const raw* const KP = (const raw*)a.KP + (long)hk * a.kp_head;
+  const raw* const VP = (const raw*)a.VP + (long)hk * a.vp_head;
+  const raw* const K = (const raw*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;
+  const raw* const V = (const raw*)a.V + (long)s.kbeg * a.v_row + (long)hk * a.v_head;
+  auto valid_of = [&](int t) { return t < np ? prefix - t * KT : kend - (t - np) * KT; };
+  tk.place(t0 < np ? a.kp_row : a.k_row, tid);   // (the prefix may have other strides: placed again at the border)
+  tv.place(t0 < np ? a.vp_row : a.v_row, tid);
+  auto load_k = [&](int t) {
+    const bool p = t < np;
+    if (t == np) tk.place(a.k_row, tid);
+    tk.load((p ? KP : K) + (long)(p ? t : t - np) * KT * (p ? a.kp_row : a.k_row), p ? a.kp_row : a.k_row, valid_of(t), dh, tid);
+  };
+  auto load_v = [&](int t) {
+    const bool p = t < np;
+    if (t == np) tv.place(a.v_row, tid);
+    tv.load((p ? VP : V) + (long)(p ? t : t - np) * KT * (p ? a.vp_row : a.v_row), p ? a.vp_row : a.v_row, valid_of(t), dh, tid);
+  };
+  auto stage = [&](int t) { return (t - t0) % 3; };
+  auto hold = [](auto& tile) {   // a tile on its way waits in the accumulation registers
+#pragma unroll
+    for (int i = 0; i < tile.NCH; ++i)
+      if constexpr (ACC) asm volatile("" : "+a"(*(u32x4*)&tile.r[i]));
+  };
+  f32x16 S[2][NJ];   // [step parity][row block]
+  bf16x8 P[2][NJ][2];   // [step parity][row block][16 keys]
+#pragma unroll
+  for (int j = 0; j < NJ; ++j)
+#pragma unroll
+    for (int st = 0; st < 2; ++st) P[1][j][st] = bf16x8{};
+
+  if (t0 < t1) {
+    // tile t0 of both, tile t0 + 1 of K; zeros where the first step's products with P = 0 read V
+    load_k(t0);
+    load_v(t0);
+    for (int i = tid; i < TV / 8; i += NT) *(uint4*)(Vs + 2 * TV + i * 8) = make_uint4(0, 0, 0, 0);
+    tk.store(Ks, LDK, valid_of(t0), dh, tid);
+    tv.store(Vs, LDV, valid_of(t0), dh, tid);
+    if (t0 + 1 < t1) {
+      load_k(t0 + 1);
+      load_v(t0 + 1);
+      tk.store(Ks + TK, LDK, valid_of(t0 + 1), dh, tid);
+    }
+    if (t0 + 2 < t1) load_k(t0 + 2);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) S[0][j] = zero16();
+#pragma unroll
+    for (int kk = 0; kk < NKD; ++kk) {
+      const bf16x8 kf = row_frag(&Ks[r * LDK + kk * 16 + 8 * g]);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) S[0][j] = mma32(kf, qf[j][kk], S[0][j]);
+    }
+  }
+  // one step: PAR its parity; Kn the next step's 32 keys, Vp the previous step's.  The matrix instructions come in slots of two (the row blocks)
+  // that share a fragment, read three slots ahead; a slot's share of the softmax is issued behind them.  First the maximum, over the first SM
+  // slots, then the exponentials.
+  constexpr int NF = NKD + 2 * NDB, NS = NJ * NF, SM = NS / 4, AHEAD = 3;
+  auto step = [&](int st_, auto par, const raw* Kn, const raw* Vp) {
+    constexpr int PAR = decltype(par)::value;
+    const int t = st_ >> 1, valid = valid_of(t) - 32 * PAR, k0 = (t - np) * KT + 32 * PAR;
+    const bool masked = a.causal && t >= np;
+    // the products leave S in accumulation registers; Q and O stay there, which leaves the others to the softmax
+    f32x16 sv[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      sv[j] = S[PAR][j];
+      if constexpr (ACC) {
+        asm volatile("" : "+v"(sv[j]));
+#pragma unroll
+        for (int kk = 0; kk < NKD; ++kk) asm volatile("" : "+a"(qf[j][kk]));
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) asm volatile("" : "+a"(o[j][d]));
+      }
+    }
+    if (valid < 32 || (masked && k0 + 31 > wq_first)) {   // wave-uniform
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int lim = (masked ? min(valid - 1, tok[j] + off - k0) : valid - 1) - 4 * g;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (8 * (i >> 2) + (i & 3) > lim) sv[j][i] = -INFINITY;
+      }
+    }
+    auto fragment = [&](int q) {
+      const int i = q / 2;   // in turn: the score products are one chain, each waits for the one before it
+      return q % 2 == 0 ? row_frag(&Kn[r * LDK + i * 16 + 8 * g]) : col_frag(Vp, LDV, 16 * (i / NDB) + 4 * g, 16 * (i / NDB) + 4 * g + 8, i % NDB * 32, lane);
+    };
+    bf16x8 f[NF];
+    float mt[NJ], mb[NJ], alpha[NJ], ps[NJ], p[NJ][16];
+    bool any = false;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) ps[j] = 0.f;
+#pragma unroll
+    for (int q = 0; q < AHEAD; ++q) f[q] = fragment(q);
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      const int q = u / NJ, h = u % NJ;
+      if (h == 0 && q + AHEAD < NF) f[q + AHEAD] = fragment(q + AHEAD);
+      const int i = q / 2;
+      if (q % 2 == 0)
+        S[PAR ^ 1][h] = mma32(f[q], qf[h][i], i == 0 ? zero16() : S[PAR ^ 1][h]);
+      else
+        o[h][i % NDB] = mma32(f[q], P[PAR ^ 1][h][i / NDB], o[h][i % NDB]);
+      if (u < SM) {
+        // maximum over elements 16 u / SM .. of both row blocks
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          if (u == 0) mt[j] = sv[j][0];
+#pragma unroll
+          for (int e = 16 * u / SM; e < 16 * (u + 1) / SM; ++e) mt[j] = fmaxf(mt[j], sv[j][e]);
+          if (u == SM - 1) {
+            mt[j] = half_max(mt[j]) * sc;
+            const bool moved = mt[j] > m[j] + 8.f;
+            any |= moved;
+            const float mn = moved ? mt[j] : m[j];
+            mb[j] = mn == -INFINITY ? 0.f : mn;
+            alpha[j] = moved ? __builtin_amdgcn_exp2f(m[j] - mn) : 1.f;   // m = -inf: 0
+            m[j] = mn;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int e = 16 * NJ * (u - SM) / (NS - SM); e < 16 * NJ * (u + 1 - SM) / (NS - SM); ++e) {
+          const int j = e / 16, c = e % 16;
+          p[j][c] = __builtin_amdgcn_exp2f(fmaf(sv[j][c], sc, -mb[j]));   // masked: 0
+          ps[j] += p[j][c];
+          // P is rounded to bf16 for its product; the sum keeps 32 bits
+          if (c % 8 == 7) {
+            pack_frag(P[PAR][j][c / 8], &p[j][c - 7]);
+            asm volatile("" : "+v"(P[PAR][j][c / 8]));   // here, not where the next step reads it
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(ps[j]));
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) l[j] = fmaf(l[j], alpha[j], ps[j]);
+    if (__ballot(any)) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int d = 0; d < NDB; ++d) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[j][d][i] *= alpha[j];
+          if constexpr (ACC) asm volatile("" : "+a"(o[j][d]));   // 16 at a time, or the compiler asks for 128 registers at once
+        }
+    }
+  };
+  // tile t + 1 of V and t + 2 of K (requested a trip ago) go into their stages, and the next ones start to travel
+  auto move = [&](int t) {
+    if (t > t0) __syncthreads();
+    if (t + 1 < t1) {
+      hold(tv);
+      tv.store(Vs + stage(t + 1) * TV, LDV, valid_of(t + 1), dh, tid);
+    }
+    if (t + 2 < t1) {
+      hold(tk);
+      tk.store(Ks + stage(t + 2) * TK, LDK, valid_of(t + 2), dh, tid);
+      load_v(t + 2);
+    }
+    if (t + 3 < t1) load_k(t + 3);
+  };
+  for (int t = t0; t < tend; ++t) {
+    move(t);
+    const raw *const Kt = Ks + stage(t) * TK, *const Vt = Vs + stage(t) * TV;
+    step(2 * t, std::integral_constant<int, 0>{}, Kt + 32 * LDK, Vs + (t - t0 + 2) % 3 * TV + 32 * LDV);
+    step(2 * t + 1, std::integral_constant<int, 1>{}, Ks + stage(t + 1) * TK, Vt);
+  }
+  if (tend > t0) {   // the last step's products with V
+    const raw* Vp = Vs + stage(tend - 1) * TV + 32 * LDV;
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int d = 0; d < NDB; ++d) {
+        const bf16x8 vf = col_frag(Vp, LDV, 16 * st + 4 * g, 16 * st + 4 * g + 8, d * 32, lane);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) o[j][d] = mma32(vf, P[1][j][st], o[j][d]);
+      }
+  }
+  for (int t = max(tend, t0); t < t1; ++t) move(t);   // (tiles that only the other waves' rows see)
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    float lt = l[j];
+    lt += __shfl_xor(lt, 32, 64);
+    if (wr + j * 32 + r >= rows) continue;
+    const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
+    const float lse = lt == 0.f ? -INFINITY : (m[j] + log2f(lt)) * 0.69314718055994530942f;
+    if (a.nsplit) {
+      const long at = (long)(a.part0 + split) * a.total_q * a.H + (long)(s.qbeg + tok[j]) * a.H + head[j];
+      if (g == 0) a.pl[at] = lse;
+      store_row<float, 16, NDB>(a.po + at * a.dhp, o[j], inv, g, dh);
+    } else {
+      if (g == 0 && a.lse) a.lse[(long)head[j] * a.total_q + s.qbeg + tok[j]] = lse;
+      store_row<bf16_t, AL, NDB>((raw*)a.O + (long)(s.qbeg + tok[j]) * a.o_row + (long)head[j] * a.o_head, o[j], inv, g, dh);
+    }
+  }
+}
+
+template <typename T, int DH, int AL>
+static void launch_fwd_al(const PackedAttn& a, dim3 grid, hipStream_t s) {
+  if constexpr (DH <= 128 && sizeof(T) == 2) {
+    if (a.groups == 4) {
+      packed_fwd_long_kernel<DH, AL, 1, 8><<<grid, 512, 0, s>>>(a);
       return;
     }
   }
-  packed_fwd_kernel<T, DH, sizeof(T)><<<grid, 256, 0, s>>>(a);
+  if constexpr (DH <= 128) {
+    if (a.groups == 2) {
+      packed_fwd_kernel<T, DH, AL, 2><<<grid, 512, 0, s>>>(a);
+      return;
+    }
+  }
+  packed_fwd_kernel<T, DH, AL, 1><<<grid, 256, 0, s>>>(a);
+}
+template <typename T, int DH>
+static void launch_fwd(const PackedAttn& a, int align, dim3 grid, hipStream_t s) {
+  if (align == 16) return launch_fwd_al<T, DH, 16>(a, grid, s);
+  if constexpr (sizeof(T) == 2) {
+    if (align == 8) return launch_fwd_al<T, DH, 8>(a, grid, s);
+  }
+  launch_fwd_al<T, DH, sizeof(T)>(a, grid, s);
 }
 template <typename T>
 static void launch_fwd_t(const PackedAttn& a, int align, dim3 grid, hipStream_t s) {
@@ -185,7 +527,8 @@ static void launch_fwd_t(const PackedAttn& a, int align, dim3 grid, hipStream_t 
 }
 void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s) {
   const long rows = (long)a.total_q * a.G;
-  const long slots = a.flat ? (rows + PACKED_BM - 1) / PACKED_BM : packed_slots(rows, PACKED_BM, a.nseq);
+  const int bm = a.groups == 4 ? PACKED_BM2 : PACKED_BM;
+  const long slots = a.flat ? (rows + bm - 1) / bm : a.levels ? (long)a.levels * a.nseq : packed_slots(rows, bm, a.nseq);
   const dim3 grid((unsigned)(slots * a.Hk * (a.nsplit > 0 ? a.nsplit : 1)));
   if (bf16)
     launch_fwd_t<bf16_t>(a, align, grid, s);

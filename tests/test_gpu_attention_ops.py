@@ -298,19 +298,22 @@ def test_infinite_and_large_logits():
     close("O", got["O"], p.reference()["O"], "f32")
 
 
-def test_hints_do_not_change_what_is_computed():
-    """max_k only splits the work; max_q cuts sequences."""
+def test_bounds_on_the_lengths():
+    """Larger bounds than the lengths only split the work otherwise; smaller ones cut the sequences."""
     p = Packed(4, 2, 64, "f32", [1, 1, 1], [700, 3, 2500], seed=19)
     ref = p.reference()
-    for mk in (0, 1, 100, 5000):
+    for mk in (2500, 3203, 100000):
         got = p.run(max_k=mk)
         close("O", got["O"], ref["O"], "f32")
         close("lse", got["lse"], ref["lse"], "f32")
-    p = Packed(4, 2, 64, "f32", [40, 2, 60], seed=20)
-    got, ref = p.run(max_q=5), p.reference()
-    for i, n in enumerate(p.nq):
-        a = p.qoff[i]
-        assert torch.all(got["O"][a + 5:p.qoff[i + 1]] == 777.0)
+    p = Packed(4, 2, 64, "f32", [40, 2, 60], [700, 3, 2500], seed=20)
+    for mq, mk in ((5, 2500), (60, 200), (5, 90)):
+        got = p.run(backward=True, max_q=mq, max_k=mk)
+        cut = Packed(4, 2, 64, "f32", [min(n, mq) for n in p.nq], [min(n, mk) for n in p.nk], seed=20)
+        cut.q, cut.k, cut.v, cut.dO, cut.qoff, cut.koff = p.q, p.k, p.v, p.dO, p.qoff, p.koff
+        ref = cut.reference(backward=True)
+        for n in ("O", "lse", "dQ", "dK", "dV"):   # 777: rows that were cut off are left
+            close(n, got[n], ref[n], "f32")
 
 
 def test_offsets_out_of_range_stay_inside():
