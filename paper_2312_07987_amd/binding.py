@@ -204,15 +204,27 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
+_torch = None
+
+
 def _launch(fn, device, stream, *args):
     """Calls fn(*args, stream) with `device` current: its current stream where none is given."""
-    import torch
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    cuda = _torch.cuda
     if device.type != "cuda":
         raise SwitchHeadError(SH_ERR_INVALID_ARG, "the tensors must be on a GPU")
-    if device.index is not None and device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            return _check(fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else int(stream)))
-    _check(fn(*args, torch.cuda.current_stream().cuda_stream if stream is None else int(stream)))
+    here = cuda.current_device()
+    if device.index is not None and device.index != here:
+        with cuda.device(device):
+            return _check(fn(*args, cuda.current_stream().cuda_stream if stream is None else int(stream)))
+    if stream is None:
+        stream = _torch._C._cuda_getCurrentRawStream(here)
+    code = fn(*args, int(stream))
+    if code != SH_OK:
+        _check(code)
 
 
 def _dtype_code(t):

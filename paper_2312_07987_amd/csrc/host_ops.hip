@@ -177,17 +177,19 @@ BwdPlan plan_backward(const AttnPlan& p) {
   BwdPlan b{};
   const long rows = (long)a.max_q * p.G, w = packed_width(a.d_head);
   size_t off = align_up((size_t)a.total_q * a.nheads * 4) + 256;
-  b.rchunk = (int)(rows > 0 ? (rows + 31) / 32 * 32 : 32);
+  b.rchunk = (int)(rows > 0 ? ceil_div(rows, PACKED_QT) * PACKED_QT : PACKED_QT);
   b.rparts = 1;
   if (a.dtype == SH_BF16 && a.d_head <= 128 && rows > 0) {
-    // Rows of a dK / dV work-group: about what a CU gets if the key tiles, a third of a rectangle of the longest rows each, were dealt evenly,
-    // so that no work-group is much longer than that; at least 512, where a work-group is about as long as its start and the extra parts.
+    // Rows of a dK / dV work-group: what a CU would get if every key tile were seen by the longest rows there are.  Parts cost their writing and a second
+    // kernel, so they are for launches with a few tiles far longer than the rest.  A step with 100 / 50 / 35 / 20 per cent of this, us: 16384 tokens
+    // of 4 heads of 128, longest 4096, 334 (no parts) / 366 / 366 / 394; 6600 tokens of 20 heads over 4, longest 4096, 688 / 719 / 709 / 714 (860 without
+    // parts).  At least 512, where a work-group is about as long as its start and the extra parts.
     const long tiles = ceil_div(a.total_k, PACKED_KB) * a.nkv_heads;
-    long chunk = tiles * rows * 35 / 100 / 256;
-    chunk = ceil_div(chunk < 512 ? 512 : chunk, 32) * 32;
+    long chunk = tiles * rows / 256;
+    chunk = ceil_div(chunk < 512 ? 512 : chunk, PACKED_QT) * PACKED_QT;
     if (chunk < rows) {
       b.rparts = (int)ceil_div(rows, chunk);
-      b.rchunk = (int)(ceil_div(ceil_div(rows, b.rparts), 32) * 32);
+      b.rchunk = (int)(ceil_div(ceil_div(rows, b.rparts), PACKED_QT) * PACKED_QT);
       b.rparts = (int)ceil_div(rows, b.rchunk);
     }
     if (b.rparts > 1) {
@@ -296,8 +298,8 @@ QkNormArgs norm_args(const sh_qk_norm& a, const void* Q, const void* K, const vo
   return n;
 }
 size_t norm_bytes(const sh_qk_norm& a) {
-  const QkNormGrid g = qk_norm_grid(a.tokens > 0 ? a.tokens : 1, a.nheads + a.nkv_heads, a.d_head, a.dtype == SH_BF16);
-  return align_up((size_t)g.x * g.y * 2 * a.d_head * 4);
+  const QkNormGrid g = qk_norm_grid(a.tokens > 0 ? a.tokens : 1, a.nheads, a.nkv_heads, a.d_head, a.dtype == SH_BF16);
+  return align_up((size_t)g.x * g.y * a.d_head * 4);
 }
 
 }  // namespace

@@ -57,7 +57,7 @@ struct PackedAttnBwd {
   // bf16, head widths 33 .. 128: score gradients dS^T [kv head][key][row of the sequence], rows of ds_ld, or NULL: computed again for dQ
   void* dS;
   long ds_ld;
-  // rows of a dK / dV work-group (a multiple of 32): key tiles that see more leave fp32 parts, [part][slot * Hk + kv head][dV, dK] of
+  // rows of a dK / dV work-group (a multiple of PACKED_QT): key tiles that see more leave fp32 parts, [part][slot * Hk + kv head][dV, dK] of
   // dkv_floats each, for a second kernel
   int rchunk, rparts;
   int klevels;                         // as levels, of the key tiles
@@ -360,16 +360,16 @@ struct QkNormArgs {
   const void* dy[2];
   void* dx[2];
   float* dw[2];
-  float* part;             // [work-groups][2][dh]
+  float* part;             // [work-groups][dh]
   long tokens, x_row[2], x_head[2], y_row[2], y_head[2];   // gradients lie as their tensors do
   int H[2], dh, rope_dim, hchunk;
   float eps;
   double rate[7];          // theta^(-2 2^k / rope_dim)
 };
 struct QkNormGrid {
-  int x, y, hchunk;
+  int x, y, yq, hchunk;   // y: head ranges of the queries (yq) and of the keys
 };
-QkNormGrid qk_norm_grid(long tokens, int heads, int dh, int bf16);
+QkNormGrid qk_norm_grid(long tokens, int H0, int H1, int dh, int bf16);
 void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipStream_t s);
 
 // launchers
@@ -378,7 +378,7 @@ void launch_packed_few(const PackedAttn& a, int bf16, int align, hipStream_t s);
 void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s);
 void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta, hipStream_t s);
 
-enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128 };
+enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128, PACKED_QT = 64 };
 // head width that a work-group's tiles are laid out for
 static inline int packed_width(int dh) { return dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
 // slots of `rows` rows in tiles of bm over nseq sequences

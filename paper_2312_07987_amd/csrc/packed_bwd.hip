@@ -180,124 +180,170 @@ __device__ __forceinline__ bool key_tile(const PackedAttnBwd& b, int id, int& nt
 
 // The same for bf16 heads of 33 .. 128 elements with two kinds of waves.  A single wave per SIMD, which is all that the kernel above has registers
 // for, leaves the matrix cores idle during exponentials, conversions and LDS traffic.  Here waves 0 .. 3 (score) hold the K and V fragments
-// of 32 keys each, form P and dS of a tile of 32 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
-// 4 .. 7 (gradient) hold the dK and dV accumulators of the same keys, add the previous tile's products, and move the row tiles from memory to
-// LDS.  One of each kind per SIMD; three stages for the row tiles (written a trip ahead, read by the score waves in the next
-// trip and by the gradient waves in the one after), two buffers for the fragments, one barrier per trip.
+// of 32 keys each, form P and dS of a tile of 64 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
+// 4 .. 7 (gradient) hold the dK and dV accumulators, add the previous tile's products, and move the row tiles from memory to LDS.  One of each
+// kind per SIMD; three stages for the row tiles (written a trip ahead, read by the score waves in the next trip and by the gradient waves
+// in the one after), two hand-over buffers, one barrier per 64 rows.  A score wave has four chains of products in flight (two blocks of 32
+// rows, S and dP): with one block per trip the chain barrier, fragment reads, products, exponentials, barrier was what a trip waited for.
+// A gradient wave owns 64 keys and half of d where d has an even number of 32-wide blocks, so that a fragment serves two products.
+// (Q and dO straight from memory in operand order for the score waves: 32 rows of 32 bytes an instruction are more than the vector memory path
+// carries, dK / dV of 16384 tokens 180 -> 329 us.)
+// Heads of 97 .. 128: rows of 256 bytes whose 16-byte pieces are permuted by the row (swizzle), so that both the 16 rows of a fragment read and the
+// 4 rows x 64 bytes of a transposing read fall on all banks, and three stages and two buffers fill the 160 KB.  Narrower ones are padded.
 // Under a causal mask the first keys of a sequence are seen by all of its rows, the last by few, so rows are cut into ranges of rchunk
 // and a (key tile, range) is a work-group; ranges that are the only one of their tile write dK and dV, others fp32 parts.
 template <int DH, int AL>
 __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) {
   const PackedAttn& a = b.f;
-  constexpr int QT = 32, KB = PACKED_KB, NST = 3, LD = DH + 16, NKD = DH / 16, NDB = DH / 32, CPR = DH / 8, TOTAL = QT * CPR, NCH = (TOTAL + 255) / 256;
+  constexpr int QT = PACKED_QT, KB = PACKED_KB, LD = DH == 128 ? 128 : DH + 16, NST = 3, NKD = DH / 16, NDB = DH / 32, CPR = DH / 8, TOTAL = QT * CPR, NCH = (TOTAL + 255) / 256;
+  constexpr bool HALF = NDB % 2 == 0;                      // a gradient wave: 64 keys x half of d, or 32 keys x all of d
+  constexpr int KBW = HALF ? 2 : 1, DW = HALF ? NDB / 2 : NDB;
   constexpr int STAGE = 2 * QT * LD;
   __shared__ __attribute__((aligned(16))) unsigned short tiles[NST * STAGE];
-  __shared__ __attribute__((aligned(16))) uint4 hand[2][4][4][64];   // [buffer][key block][P st 0, P st 1, dS st 0, dS st 1][lane]
-  __shared__ __attribute__((aligned(16))) float lse_s[NST][QT], del_s[NST][QT];
+  __shared__ __attribute__((aligned(16))) uint4 hand[2][4][8][64];   // [buffer][key block][P, dS of 16 rows in turn][lane]
+  static_assert(sizeof tiles + sizeof hand <= 160 * 1024, "fits a CU");
 
   int bid = blockIdx.x;
   const int hk = bid % a.Hk;
   bid /= a.Hk;
-  const int nslot = gridDim.x / (a.Hk * b.rparts), part = bid / nslot, slot_ = bid % nslot;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, blk = wave & 3, r = lane & 31, g = lane >> 5, dh = a.dh;
+  const int nslot = gridDim.x / (a.Hk * b.rparts), part = b.rparts - 1 - bid / nslot, slot_ = bid % nslot;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
   int nth, slot;
   SeqGeom s;
   if (!key_tile(b, slot_, nth, slot, s)) return;
   const int k0 = nth * KB;
   if (k0 >= s.lk) return;
-  const int off = s.lk - s.lq, rows = s.lq * a.G, key = k0 + blk * 32 + r, wk_first = k0 + blk * 32;
+  const int off = s.lk - s.lq, rows = s.lq * a.G;
   const int first = a.causal ? max(k0 - off, 0) * a.G / QT * QT : 0;   // the first row tile that sees one of the keys
   // this range of the rows, and whether it is the only one
   const int p0 = min(first, max(rows - 1, 0)) / b.rchunk, p1 = max(rows - 1, 0) / b.rchunk;
   if (part < p0 || part > p1) return;
   const int rbeg = max(first, part * b.rchunk), rend = min(rows, (part + 1) * b.rchunk);
   const int n = rbeg < rend ? (rend - rbeg + QT - 1) / QT : 0;
+  auto place = [&](int row, int& tok, int& head) {
+    tok = div_by(row, a.g_inv);
+    head = hk * a.G + row - tok * a.G;
+    tok += s.qbeg;
+  };
+
+  // where piece p of a tile's row lies
+  auto piece = [](int row, int p) { return DH == 128 ? p ^ ((row & 3) << 2 | (row >> 2 & 1) << 1 | (row >> 3 & 1)) : p; };
 
   if (wave < 4) {
+    const int key = k0 + wave * 32 + r, wk_first = k0 + wave * 32;
     bf16x8 kf[NKD], vf[NKD];
-    const unsigned short* K = (const unsigned short*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head;
-    const unsigned short* V = (const unsigned short*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head;
-    mem_frags<bf16_t, AL, NKD, 16>(kf, K, 8 * g, dh, key < s.lk);
-    mem_frags<bf16_t, AL, NKD, 16>(vf, V, 8 * g, dh, key < s.lk);
+    mem_frags<bf16_t, AL, NKD, 16>(kf, (const raw16*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head, 8 * g, dh, key < s.lk);
+    mem_frags<bf16_t, AL, NKD, 16>(vf, (const raw16*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head, 8 * g, dh, key < s.lk);
     // (keys past the sequence have no row of dS^T: they repeat the last key's address and do not store)
-    unsigned short* dsrow = nullptr;
-    if (b.dS) dsrow = (unsigned short*)b.dS + ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 4 * g;
+    raw16* const dsrow = (raw16*)b.dS + (b.dS ? ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 4 * g : 0);
     const bool ds_store = b.dS && key < s.lk;
     const float sc = a.scale * 1.44269504088896340736f;
+    // the statistics of the next tile's rows (lane half 0: lse, 1: delta; rows past the end repeat the last one)
+    float st[QT / 32];
+    auto statistics = [&](int r0) {
+#pragma unroll
+      for (int blk = 0; blk < QT / 32; ++blk) {
+        int tok, head;
+        place(min(r0 + blk * 32 + r, rows - 1), tok, head);
+        st[blk] = (g ? b.delta : a.lse)[(long)head * a.total_q + tok];
+      }
+    };
+    if (n > 0) statistics(rbeg);
     for (int it = 0; it <= n; ++it) {
       __syncthreads();
       if (it == n) break;
-      const int r0 = rbeg + it * QT;
-      const unsigned short* Qr = tiles + (it % NST) * STAGE;
-      const unsigned short* Gr = Qr + QT * LD;
-      f32x16 S = zero16(), dP = zero16();
+      const raw16* Qr = tiles + it % NST * STAGE;
+      const raw16* Gr = Qr + QT * LD;
+      // the statistics go through the start of the wave's own hand-over place, which is not written before they are read
+      uint4* const place_ = hand[it & 1][wave][0];
+      float* const sl = (float*)place_;
 #pragma unroll
-      for (int kk = 0; kk < NKD; ++kk) {
-        S = mma32(row_frag(&Qr[r * LD + kk * 16 + 8 * g]), kf[kk], S);
-        dP = mma32(row_frag(&Gr[r * LD + kk * 16 + 8 * g]), vf[kk], dP);
-      }
-      float p[16], ds[16];
-      const float* Ls = lse_s[it % NST];
-      const float* Ds = del_s[it % NST];
-      // wave-uniform: most tiles lie wholly inside the visible region
-      const bool masked = r0 + QT > rend || wk_first + 32 > s.lk || (a.causal && wk_first + 31 > div_by(r0, a.g_inv) + off);
+      for (int blk = 0; blk < QT / 32; ++blk) sl[(blk * 2 + g) * 32 + r] = g ? st[blk] : st[blk] * 1.44269504088896340736f;
+      if (it + 1 < n) statistics(rbeg + (it + 1) * QT);
+      f32x16 S_[QT / 32], dP_[QT / 32];
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        const f32x4 L = *(const f32x4*)&Ls[8 * i4 + 4 * g], D = *(const f32x4*)&Ds[8 * i4 + 4 * g];
+      for (int blk = 0; blk < QT / 32; ++blk) S_[blk] = dP_[blk] = zero16();
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const int i = 4 * i4 + t;
-          p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L[t]));
-          ds[i] = p[i] * (dP[i] - D[t]);
+      for (int kk = 0; kk < NKD; ++kk)
+#pragma unroll
+        for (int blk = 0; blk < QT / 32; ++blk) {
+          const int at = (blk * 32 + r) * LD + piece(r, 2 * kk + g) * 8;
+          S_[blk] = mma32(row_frag(Qr + at), kf[kk], S_[blk]);
+          dP_[blk] = mma32(row_frag(Gr + at), vf[kk], dP_[blk]);
         }
-      }
-      if (masked) {
+      wave_order();
+      f32x4 L_[QT / 32][4], D_[QT / 32][4];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int rr = r0 + 8 * (i >> 2) + 4 * g + (i & 3);
-          const bool vis = rr < rend && key < s.lk && (!a.causal || key <= div_by(rr, a.g_inv) + off);
-          p[i] = vis ? p[i] : 0.f;
-          ds[i] = vis ? ds[i] : 0.f;
+      for (int blk = 0; blk < QT / 32; ++blk)
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          L_[blk][i4] = *(const f32x4*)&sl[blk * 64 + 8 * i4 + 4 * g];
+          D_[blk][i4] = *(const f32x4*)&sl[blk * 64 + 32 + 8 * i4 + 4 * g];
         }
-      }
-      uint4* hd = hand[it & 1][blk][0] + lane;
+      wave_order();
 #pragma unroll
-      for (int st = 0; st < 2; ++st) {
-        union {
-          bf16x8 v;
-          uint4 q;
-          uint2 hh[2];
-        } up, ud;
-        pack_frag(up.v, &p[8 * st]);
-        pack_frag(ud.v, &ds[8 * st]);
-        hd[st * 64] = up.q;
-        hd[(2 + st) * 64] = ud.q;
-        if (ds_store) {   // elements 0..3 / 4..7: rows r0 + 16 st + 4 g + {0..3} / + 8 + {0..3} of this lane's key
-          *(uint2*)(dsrow + r0 + 16 * st) = ud.hh[0];
-          *(uint2*)(dsrow + r0 + 16 * st + 8) = ud.hh[1];
+      for (int blk = 0; blk < QT / 32; ++blk) {
+        const int r0 = rbeg + it * QT + blk * 32;
+        if (r0 >= rend) break;   // uniform
+        const f32x16 S = S_[blk], dP = dP_[blk];
+        float p[16], ds[16];
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+          const f32x4 L = L_[blk][i4], D = D_[blk][i4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const int i = 4 * i4 + t;
+            p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L[t]));
+            ds[i] = p[i] * (dP[i] - D[t]);
+          }
+        }
+        // wave-uniform: most blocks lie wholly inside the visible region
+        if (r0 + 32 > rend || wk_first + 32 > s.lk || (a.causal && wk_first + 31 > div_by(r0, a.g_inv) + off)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int rr = r0 + 8 * (i >> 2) + 4 * g + (i & 3);
+            const bool vis = rr < rend && key < s.lk && (!a.causal || key <= div_by(rr, a.g_inv) + off);
+            p[i] = vis ? p[i] : 0.f;
+            ds[i] = vis ? ds[i] : 0.f;
+          }
+        }
+        // P and dS are rounded to bf16 here, once, for their products
+        uint4* hd = hand[it & 1][wave][blk * 4] + lane;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          union {
+            bf16x8 v;
+            uint4 q;
+            uint2 hh[2];
+          } up, ud;
+          pack_frag(up.v, &p[8 * h]);
+          pack_frag(ud.v, &ds[8 * h]);
+          hd[2 * h * 64] = up.q;
+          hd[(2 * h + 1) * 64] = ud.q;
+          if (ds_store) {   // elements 0..3 / 4..7: rows r0 + 16 h + 4 g + {0..3} / + 8 + {0..3} of this lane's key
+            *(uint2*)(dsrow + r0 + 16 * h) = ud.hh[0];
+            *(uint2*)(dsrow + r0 + 16 * h + 8) = ud.hh[1];
+          }
         }
       }
     }
     return;
   }
 
-  const int gt = tid - 256;
+  const int gt = tid - 256, gw = wave - 4;
+  const int kb0 = HALF ? (gw & 1) * 2 : gw, d0 = HALF ? (gw >> 1) * DW : 0;   // the wave's key blocks and d blocks
   uint4 tq[NCH], tg[NCH];
-  float nlse = 0.f, ndel = 0.f;
   auto prefetch = [&](int r0) {   // (rows past the end repeat the last one)
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int c = gt + i * 256, row = min(r0 + c / CPR, rows - 1), d = c % CPR * 8;
-      const int tok = div_by(row, a.g_inv), head = hk * a.G + row - tok * a.G;
-      tq[i] = load_row_piece<bf16_t, AL>((const unsigned short*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head, d, dh);
-      tg[i] = load_row_piece<bf16_t, AL>((const unsigned short*)b.dO + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head, d, dh);
+      const int c = gt + i * 256, d = c % CPR * 8;
+      int tok, head;
+      place(min(r0 + c / CPR, rows - 1), tok, head);
+      tq[i] = load_row_piece<bf16_t, AL>((const raw16*)a.Q + (long)tok * a.q_row + (long)head * a.q_head, d, dh);
+      tg[i] = load_row_piece<bf16_t, AL>((const raw16*)b.dO + (long)tok * a.o_row + (long)head * a.o_head, d, dh);
     }
-    const int row = min(r0 + (gt & (QT - 1)), rows - 1), tok = div_by(row, a.g_inv), head = hk * a.G + row - tok * a.G;
-    nlse = a.lse[(long)head * a.total_q + s.qbeg + tok];
-    ndel = b.delta[(long)head * a.total_q + s.qbeg + tok];
   };
-  auto stage = [&](int st, int r0) {
-    unsigned short* t = tiles + st * STAGE;
+  auto stage = [&](raw16* t, int r0) {
     const bool whole = r0 + QT <= rows && dh == DH;   // uniform
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
@@ -309,65 +355,85 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
         x = cut_piece<bf16_t, AL>(x, d, dh);
         if (r0 + row >= rows) q = x = make_uint4(0, 0, 0, 0);
       }
-      *(uint4*)(t + row * LD + d) = q;
-      *(uint4*)(t + (QT + row) * LD + d) = x;
-    }
-    if (gt < QT) {
-      lse_s[st][gt] = nlse * 1.44269504088896340736f;
-      del_s[st][gt] = ndel;
+      *(uint4*)(t + row * LD + piece(row, d / 8) * 8) = q;
+      *(uint4*)(t + (QT + row) * LD + piece(row, d / 8) * 8) = x;
     }
   };
-  f32x16 accK[NDB], accV[NDB];
+  // rows k .. k + 3 and k + 8 .. k + 11 (k = 16 h + 4 g) of column 32 d + lane % 32
+  auto columns = [&](const raw16* tile, int h, int d) {
+    const int q = lane & 15, row = 16 * h + 4 * g + (q >> 2), p = 4 * d + (lane >> 4 & 1) * 2 + (q >> 1 & 1), in = (q & 1) * 4;
+    union {
+      s16x4 half[2];
+      bf16x8 v;
+    } u;
+    u.half[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, tile + row * LD + piece(row, p) * 8 + in));
+    u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, tile + (row + 8) * LD + piece(row + 8, p) * 8 + in));
+    return u.v;
+  };
+  f32x16 accK[KBW][DW], accV[KBW][DW];
 #pragma unroll
-  for (int d = 0; d < NDB; ++d) accK[d] = accV[d] = zero16();
+  for (int k = 0; k < KBW; ++k)
+#pragma unroll
+    for (int d = 0; d < DW; ++d) accK[k][d] = accV[k][d] = zero16();
   if (n > 0) {
     prefetch(rbeg);
-    stage(0, rbeg);
+    stage(tiles, rbeg);
     if (n > 1) prefetch(rbeg + QT);
   }
   for (int it = 0; it <= n; ++it) {
     __syncthreads();
     // the tile it + 1 (requested a trip ago) goes into its stage and the tile it + 2 starts to travel
     if (it + 1 < n) {
-      stage((it + 1) % NST, rbeg + (it + 1) * QT);
+      stage(tiles + (it + 1) % NST * STAGE, rbeg + (it + 1) * QT);
       if (it + 2 < n) prefetch(rbeg + (it + 2) * QT);
     }
     if (it == 0) continue;
-    const unsigned short* Qt = tiles + ((it - 1) % NST) * STAGE;
-    const unsigned short* Gt = Qt + QT * LD;
-    const uint4* hd = hand[(it - 1) & 1][blk][0] + lane;
+    const raw16* Qt = tiles + (it - 1) % NST * STAGE;
+    const raw16* Gt = Qt + QT * LD;
+    const int left = rend - (rbeg + (it - 1) * QT);   // rows of the tile that exist
 #pragma unroll
-    for (int st = 0; st < 2; ++st) {
+    for (int h = 0; h < QT / 16; ++h) {
+      if ((h & ~1) * 16 >= left) break;   // uniform: blocks of 32 rows that the score waves left out
       union {
         uint4 q;
         bf16x8 v;
-      } up, ud;
-      up.q = hd[st * 64];
-      ud.q = hd[(2 + st) * 64];
-      const int kb0 = 16 * st + 4 * g;
+      } up[KBW], ud[KBW];
 #pragma unroll
-      for (int d = 0; d < NDB; ++d) {
-        accV[d] = mma32(col_frag(Gt, LD, kb0, kb0 + 8, d * 32, lane), up.v, accV[d]);
-        accK[d] = mma32(col_frag(Qt, LD, kb0, kb0 + 8, d * 32, lane), ud.v, accK[d]);
+      for (int k = 0; k < KBW; ++k) {
+        up[k].q = hand[(it - 1) & 1][kb0 + k][2 * h][lane];
+        ud[k].q = hand[(it - 1) & 1][kb0 + k][2 * h + 1][lane];
+      }
+#pragma unroll
+      for (int d = 0; d < DW; ++d) {
+        const bf16x8 gfr = columns(Gt, h, d0 + d), qfr = columns(Qt, h, d0 + d);
+#pragma unroll
+        for (int k = 0; k < KBW; ++k) {
+          accV[k][d] = mma32(gfr, up[k].v, accV[k][d]);
+          accK[k][d] = mma32(qfr, ud[k].v, accK[k][d]);
+        }
       }
     }
   }
-  if (p0 == p1) {
-    if (key < s.lk) {
-      store_row<bf16_t, AL, NDB>((unsigned short*)b.dK + (long)(s.kbeg + key) * a.k_row + (long)hk * a.k_head, accK, a.scale, g, dh);
-      store_row<bf16_t, AL, NDB>((unsigned short*)b.dV + (long)(s.kbeg + key) * a.v_row + (long)hk * a.v_head, accV, 1.f, g, dh);
+#pragma unroll
+  for (int k = 0; k < KBW; ++k) {
+    const int key = k0 + (kb0 + k) * 32 + r;
+    if (p0 == p1) {
+      if (key < s.lk) {
+        store_row<bf16_t, AL, DW>((raw16*)b.dK + (long)(s.kbeg + key) * a.k_row + (long)hk * a.k_head + d0 * 32, accK[k], a.scale, g, dh - d0 * 32);
+        store_row<bf16_t, AL, DW>((raw16*)b.dV + (long)(s.kbeg + key) * a.v_row + (long)hk * a.v_head + d0 * 32, accV[k], 1.f, g, dh - d0 * 32);
+      }
+      continue;
     }
-    return;
+    // a part: accumulators in register order, 16 bytes per lane, by key block and d block
+    f32x4* out = (f32x4*)(b.dkv + ((long)part * b.kslots + (long)slot * a.Hk + hk) * b.dkv_floats) + ((kb0 + k) * NDB + d0) * 4 * 64 + lane;
+#pragma unroll
+    for (int d = 0; d < DW; ++d)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        out[(d * 4 + i4) * 64] = f32x4{accV[k][d][4 * i4], accV[k][d][4 * i4 + 1], accV[k][d][4 * i4 + 2], accV[k][d][4 * i4 + 3]};
+        out[(4 * NDB * 4 + d * 4 + i4) * 64] = f32x4{accK[k][d][4 * i4], accK[k][d][4 * i4 + 1], accK[k][d][4 * i4 + 2], accK[k][d][4 * i4 + 3]};
+      }
   }
-  // a part: accumulators in register order, 16 bytes per lane
-  f32x4* out = (f32x4*)(b.dkv + ((long)part * b.kslots + (long)slot * a.Hk + hk) * b.dkv_floats) + blk * NDB * 4 * 64 + lane;
-#pragma unroll
-  for (int d = 0; d < NDB; ++d)
-#pragma unroll
-    for (int i4 = 0; i4 < 4; ++i4) {
-      out[(d * 4 + i4) * 64] = f32x4{accV[d][4 * i4], accV[d][4 * i4 + 1], accV[d][4 * i4 + 2], accV[d][4 * i4 + 3]};
-      out[(4 * NDB * 4 + d * 4 + i4) * 64] = f32x4{accK[d][4 * i4], accK[d][4 * i4 + 1], accK[d][4 * i4 + 2], accK[d][4 * i4 + 3]};
-    }
 }
 
 // Adds the parts of the key tiles that have several, in range order: waves 0 .. 3 dV, 4 .. 7 dK, 32 keys each
@@ -382,7 +448,7 @@ __global__ __launch_bounds__(512) void packed_dkv_join_kernel(PackedAttnBwd b) {
   if (!find_slot<true>(a, PACKED_KB, slot, nth, s)) return;
   const int k0 = nth * PACKED_KB;
   if (k0 >= s.lk) return;
-  const int off = s.lk - s.lq, rows = s.lq * a.G, first = a.causal ? max(k0 - off, 0) * a.G / 32 * 32 : 0;
+  const int off = s.lk - s.lq, rows = s.lq * a.G, first = a.causal ? max(k0 - off, 0) * a.G / PACKED_QT * PACKED_QT : 0;
   const int p0 = min(first, max(rows - 1, 0)) / b.rchunk, p1 = max(rows - 1, 0) / b.rchunk;
   if (p0 == p1) return;
   f32x16 acc[NDB];
@@ -449,7 +515,7 @@ __global__ __launch_bounds__(256, 2) void packed_dq_ds_kernel(PackedAttnBwd b) {
   }
   for (int k0 = 0; k0 < kend; k0 += KT) {
     // the first row written for this tile's keys, and the keys that exist
-    const int written = a.causal ? max(k0 / PACKED_KB * PACKED_KB - off, 0) * a.G / 32 * 32 : 0;
+    const int written = a.causal ? max(k0 / PACKED_KB * PACKED_KB - off, 0) * a.G / PACKED_QT * PACKED_QT : 0;
     const bool keep = row0 + dr >= written && row0 + dr < (rows + 31) / 32 * 32;
     __syncthreads();
     tk.store(Ks, LD, kend - k0, dh, tid);

@@ -5,8 +5,8 @@
 //   dn = dy turned back,  dw = sum over rows of dn x r,  g = dn w,  dx = r (g - x r mean(g x r)).
 //
 // Bound by bytes: x (and dy) read once, y (dx) written once.  A group of LR lanes holds a head's row in 16-byte pieces (the
-// sums over it are a butterfly), takes one token and walks that token's heads, so the token's sines and cosines are computed once for all
-// of its heads: angles in 64 bits down to a fraction of a turn and a remainder, so positions of millions keep their place to the last bit of fp32.
+// sums over it are a butterfly), takes one token and walks up to 16 of its heads, for which the token's sines and cosines are computed
+// once: angles in 64 bits down to a fraction of a turn and a remainder, so positions of millions keep their place to the last bit of fp32.
 #include "packed_attn.h"
 
 namespace sh {
@@ -64,17 +64,14 @@ __device__ __forceinline__ void store_piece(typename Elem<T>::raw* row, int d, i
 template <typename T, int AL>
 struct NormCols {
   static constexpr int N = Elem<T>::PER;
-  float w[2][N];
+  float w[N];
   double rate[N / 2];
-  __device__ __forceinline__ void init(const QkNormArgs& a, int d) {
+  __device__ __forceinline__ void init(const QkNormArgs& a, int side, int d) {
     Lane<T> l;
+    const typename Elem<T>::raw* w_ = (const typename Elem<T>::raw*)a.w[side];
+    if (w_) l.from(lane_piece<T, AL>(w_, d, a.dh));
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const typename Elem<T>::raw* w_ = (const typename Elem<T>::raw*)a.w[k];
-      if (w_) l.from(lane_piece<T, AL>(w_, d, a.dh));
-#pragma unroll
-      for (int i = 0; i < N; ++i) w[k][i] = w_ ? l.v[i] : 1.f;
-    }
+    for (int i = 0; i < N; ++i) w[i] = w_ ? l.v[i] : 1.f;
     // theta^(-2 i / rope_dim) / 2 pi from its binary powers: pair i = d / 2 + j
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) {
@@ -88,42 +85,44 @@ struct NormCols {
   }
 };
 
+// blockIdx.y: a range of hchunk heads of the queries, then of the keys
 template <typename T, int LR, int AL>
 __global__ __launch_bounds__(256) void qk_norm_rope_fwd_kernel(QkNormArgs a) {
   typedef typename Elem<T>::raw raw;
   constexpr int N = Elem<T>::PER;
-  const int d = threadIdx.x % LR * N, heads = a.H[0] + a.H[1];
-  const int h0 = blockIdx.y * a.hchunk, h1 = min(h0 + a.hchunk, heads);
+  const int d = threadIdx.x % LR * N, yq = (a.H[0] + a.hchunk - 1) / a.hchunk, side = (int)blockIdx.y >= yq;
+  const int h0 = (blockIdx.y - (side ? yq : 0)) * a.hchunk, h1 = min(h0 + a.hchunk, a.H[side]);
+  const long xh = a.x_head[side], yh = a.y_head[side];
   NormCols<T, AL> c;
-  c.init(a, d);
+  c.init(a, side, d);
   const float inv_d = 1.f / a.dh;
   for (long t = (long)blockIdx.x * (256 / LR) + threadIdx.x / LR; t < a.tokens; t += (long)gridDim.x * (256 / LR)) {
-    auto row = [&](int h) { return h < a.H[0] ? (const raw*)a.x[0] + t * a.x_row[0] + h * a.x_head[0] : (const raw*)a.x[1] + t * a.x_row[1] + (h - a.H[0]) * a.x_head[1]; };
-    uint4 next = load_row_piece<T, AL>(row(h0), d, a.dh);
+    const raw* x_ = (const raw*)a.x[side] + t * a.x_row[side] + h0 * xh;
+    raw* y_ = (raw*)a.y[side] + t * a.y_row[side] + h0 * yh;
+    uint4 next = load_row_piece<T, AL>(x_, d, a.dh);
     float cs[N / 2], sn[N / 2];
     const double pos = a.positions ? a.positions[t] : (double)t;
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) turn_cos_sin(pos * c.rate[j], cs[j], sn[j]);
-    for (int h = h0; h < h1; ++h) {
+    for (int h = h0; h < h1; ++h, y_ += yh) {
       Lane<T> x;
       x.from(cut_piece<T, AL>(next, d, a.dh));
-      if (h + 1 < h1) next = load_row_piece<T, AL>(row(h + 1), d, a.dh);
+      x_ += xh;
+      if (h + 1 < h1) next = load_row_piece<T, AL>(x_, d, a.dh);
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < N; ++i) sum = fmaf(x.v[i], x.v[i], sum);
 #pragma unroll
       for (int k = 1; k < LR; k <<= 1) sum += __shfl_xor(sum, k, 64);
       const float r = 1.f / sqrtf(fmaf(sum, inv_d, a.eps));
-      const int k = h >= a.H[0];
       float y[N];
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
-        const float u = x.v[2 * j] * r * c.w[k][2 * j], v = x.v[2 * j + 1] * r * c.w[k][2 * j + 1];
+        const float u = x.v[2 * j] * r * c.w[2 * j], v = x.v[2 * j + 1] * r * c.w[2 * j + 1];
         y[2 * j] = u * cs[j] - v * sn[j];
         y[2 * j + 1] = u * sn[j] + v * cs[j];
       }
-      raw* out = k ? (raw*)a.y[1] + t * a.y_row[1] + (h - a.H[0]) * a.y_head[1] : (raw*)a.y[0] + t * a.y_row[0] + h * a.y_head[0];
-      store_piece<T, AL>(out, d, a.dh, y);
+      store_piece<T, AL>(y_, d, a.dh, y);
     }
   }
 }
@@ -132,32 +131,35 @@ template <typename T, int LR, int AL>
 __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormArgs a) {
   typedef typename Elem<T>::raw raw;
   constexpr int N = Elem<T>::PER, NG = 256 / LR;
-  __shared__ float part[2][NG][LR * N + 1];
-  const int d = threadIdx.x % LR * N, grp = threadIdx.x / LR, heads = a.H[0] + a.H[1];
-  const int h0 = blockIdx.y * a.hchunk, h1 = min(h0 + a.hchunk, heads);
+  __shared__ float part[NG][LR * N + 1];
+  const int d = threadIdx.x % LR * N, grp = threadIdx.x / LR, yq = (a.H[0] + a.hchunk - 1) / a.hchunk, side = (int)blockIdx.y >= yq;
+  const int h0 = (blockIdx.y - (side ? yq : 0)) * a.hchunk, h1 = min(h0 + a.hchunk, a.H[side]);
+  const long xh = a.x_head[side], yh = a.y_head[side];
   NormCols<T, AL> c;
-  c.init(a, d);
+  c.init(a, side, d);
   const float inv_d = 1.f / a.dh;
-  float dw[2][N];
+  float dw[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) dw[0][i] = dw[1][i] = 0.f;
+  for (int i = 0; i < N; ++i) dw[i] = 0.f;
   for (long t = (long)blockIdx.x * NG + grp; t < a.tokens; t += (long)gridDim.x * NG) {
-    auto row = [&](int h) { return h < a.H[0] ? (const raw*)a.x[0] + t * a.x_row[0] + h * a.x_head[0] : (const raw*)a.x[1] + t * a.x_row[1] + (h - a.H[0]) * a.x_head[1]; };
-    auto drow = [&](int h) { return h < a.H[0] ? (const raw*)a.dy[0] + t * a.y_row[0] + h * a.y_head[0] : (const raw*)a.dy[1] + t * a.y_row[1] + (h - a.H[0]) * a.y_head[1]; };
-    uint4 nx = load_row_piece<T, AL>(row(h0), d, a.dh), nd = load_row_piece<T, AL>(drow(h0), d, a.dh);
+    const raw* x_ = (const raw*)a.x[side] + t * a.x_row[side] + h0 * xh;
+    raw* dx_ = (raw*)a.dx[side] + t * a.x_row[side] + h0 * xh;
+    const raw* dy_ = (const raw*)a.dy[side] + t * a.y_row[side] + h0 * yh;
+    uint4 nx = load_row_piece<T, AL>(x_, d, a.dh), nd = load_row_piece<T, AL>(dy_, d, a.dh);
     float cs[N / 2], sn[N / 2];
     const double pos = a.positions ? a.positions[t] : (double)t;
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) turn_cos_sin(pos * c.rate[j], cs[j], sn[j]);
-    for (int h = h0; h < h1; ++h) {
+    for (int h = h0; h < h1; ++h, dx_ += xh) {
       Lane<T> x, dy;
       x.from(cut_piece<T, AL>(nx, d, a.dh));
       dy.from(cut_piece<T, AL>(nd, d, a.dh));
+      x_ += xh;
+      dy_ += yh;
       if (h + 1 < h1) {
-        nx = load_row_piece<T, AL>(row(h + 1), d, a.dh);
-        nd = load_row_piece<T, AL>(drow(h + 1), d, a.dh);
+        nx = load_row_piece<T, AL>(x_, d, a.dh);
+        nd = load_row_piece<T, AL>(dy_, d, a.dh);
       }
-      const bool k = h >= a.H[0];
       float dn[N], g[N], sum = 0.f, dot = 0.f;
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormArgs a) {
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
-        g[i] = dn[i] * (k ? c.w[1][i] : c.w[0][i]);
+        g[i] = dn[i] * c.w[i];
         sum = fmaf(x.v[i], x.v[i], sum);
         dot = fmaf(g[i], x.v[i], dot);
       }
@@ -180,47 +182,42 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormArgs a) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         dx[i] = r * (g[i] - x.v[i] * coef);
-        const float e = dn[i] * x.v[i] * r;
-        dw[0][i] += k ? 0.f : e;
-        dw[1][i] += k ? e : 0.f;
+        dw[i] = fmaf(dn[i], x.v[i] * r, dw[i]);
       }
-      raw* out = k ? (raw*)a.dx[1] + t * a.x_row[1] + (h - a.H[0]) * a.x_head[1] : (raw*)a.dx[0] + t * a.x_row[0] + h * a.x_head[0];
-      store_piece<T, AL>(out, d, a.dh, dx);
+      store_piece<T, AL>(dx_, d, a.dh, dx);
     }
   }
   // the work-group's sums in group order, then one row of partial sums per work-group
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    part[0][grp][d + i] = dw[0][i];
-    part[1][grp][d + i] = dw[1][i];
-  }
+  for (int i = 0; i < N; ++i) part[grp][d + i] = dw[i];
   __syncthreads();
   const long b = (long)blockIdx.y * gridDim.x + blockIdx.x;
-  for (int i = threadIdx.x; i < 2 * a.dh; i += 256) {
-    const int k = i / a.dh, col = i % a.dh;
+  for (int i = threadIdx.x; i < a.dh; i += 256) {
     float s = 0.f;
-    for (int q = 0; q < NG; ++q) s += part[k][q][col];
-    a.part[b * 2 * a.dh + i] = s;
+    for (int q = 0; q < NG; ++q) s += part[q][i];
+    a.part[b * a.dh + i] = s;
   }
 }
 
-// dw[k][col] = the work-groups' partial sums, 32 strands of them in order, then the strands in order
-__global__ __launch_bounds__(256) void qk_norm_dw_kernel(const float* part, int blocks, int dh, float* dw0, float* dw1) {
+// dw[k][col] = the work-groups' partial sums (yq rows of `blocks` for the queries, the rest for the keys), 32 strands of them in order, then the strands in order
+__global__ __launch_bounds__(256) void qk_norm_dw_kernel(const float* part, int blocks, int yq, int yk, int dh, float* dw0, float* dw1) {
   __shared__ float s[32][9];
-  const int c = threadIdx.x & 7, q = threadIdx.x >> 3, i = blockIdx.x * 8 + c;
+  const int c = threadIdx.x & 7, q = threadIdx.x >> 3, k = blockIdx.y, i = blockIdx.x * 8 + c;
+  const int n = blocks * (k ? yk : yq);
+  const float* p = part + (long)(k ? yq : 0) * blocks * dh;
   float x = 0.f;
-  if (i < 2 * dh) {
+  if (i < dh) {
 #pragma unroll 8
-    for (int b = q; b < blocks; b += 32) x += part[(long)b * 2 * dh + i];
+    for (int b = q; b < n; b += 32) x += p[(long)b * dh + i];
   }
   s[q][c] = x;
   __syncthreads();
-  if (q == 0 && i < 2 * dh) {
+  if (q == 0 && i < dh) {
     float t = 0.f;
 #pragma unroll
     for (int j = 0; j < 32; ++j) t += s[j][c];
-    float* dw = i < dh ? dw0 : dw1;
-    if (dw) dw[i % dh] = t;
+    float* dw = k ? dw1 : dw0;
+    if (dw) dw[i] = t;
   }
 }
 
@@ -231,17 +228,18 @@ static int row_lanes(int dh, int bf16) {
   while (l * n < dh) l *= 2;
   return l;
 }
-// Work-groups along the tokens, and heads a group of lanes walks.  All heads of a token by one group computes its angles once; with few tokens the
-// heads are spread over more groups until the chip has 8 waves on every SIMD of a quarter of its CUs
-QkNormGrid qk_norm_grid(long tokens, int heads, int dh, int bf16) {
+// Work-groups along the tokens, and heads that a group of lanes walks (of one side: its columns' weights and sums are then one register each).  A
+// group's angles serve its heads, so it takes 16 of them, fewer where there are few tokens (some 2048 work-groups: 8 waves on every SIMD).
+QkNormGrid qk_norm_grid(long tokens, int H0, int H1, int dh, int bf16) {
   const int per = 256 / row_lanes(dh, bf16);
   QkNormGrid g;
   const long blocks = (tokens + per - 1) / per;
   g.x = (int)(blocks < 1024 ? blocks : 1024);
-  int parts = (int)(1024 / g.x);
-  parts = parts < 1 ? 1 : parts > heads ? heads : parts;
-  g.hchunk = (heads + parts - 1) / parts;
-  g.y = (heads + g.hchunk - 1) / g.hchunk;
+  const int want = 2048 / g.x, heads = H0 + H1;
+  g.hchunk = (heads + want - 1) / want;
+  if (g.hchunk > 16) g.hchunk = 16;
+  g.yq = (H0 + g.hchunk - 1) / g.hchunk;
+  g.y = g.yq + (H1 + g.hchunk - 1) / g.hchunk;
   return g;
 }
 
@@ -261,7 +259,7 @@ static void launch_norm_lr(const QkNormArgs& a, int align, dim3 grid, bool backw
   launch_norm_al<T, LR, sizeof(T)>(a, grid, backward, s);
 }
 void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipStream_t s) {
-  const QkNormGrid g = qk_norm_grid(a.tokens, a.H[0] + a.H[1], a.dh, bf16);
+  const QkNormGrid g = qk_norm_grid(a.tokens, a.H[0], a.H[1], a.dh, bf16);
   const dim3 grid(g.x, g.y);
   a.hchunk = g.hchunk;
   const int lr = row_lanes(a.dh, bf16);
@@ -282,7 +280,7 @@ void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipSt
     else
       launch_norm_lr<float, 64>(a, align, grid, backward, s);
   }
-  if (backward && (a.dw[0] || a.dw[1])) qk_norm_dw_kernel<<<dim3((2 * a.dh + 7) / 8), 256, 0, s>>>(a.part, g.x * g.y, a.dh, a.dw[0], a.dw[1]);
+  if (backward && (a.dw[0] || a.dw[1])) qk_norm_dw_kernel<<<dim3((a.dh + 7) / 8, 2), 256, 0, s>>>(a.part, g.x, g.yq, g.y - g.yq, a.dh, a.dw[0], a.dw[1]);
 }
 
 }  // namespace sh
