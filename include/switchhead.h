@@ -339,6 +339,49 @@ sh_status switchhead_qk_norm_rope_backward(const sh_qk_norm* a, const void* Q, c
                                            const int32_t* positions, const void* dY_Q, const void* dY_K, void* dQ, void* dK,
                                            float* dw_Q, float* dw_K, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/*
+ * The layer over packed sequences (documents of different lengths in one call; questions behind one text): the layer of
+ * switchhead_forward with B = 1 and T rows, where attention stays within each sequence.  The routers, projections and experts
+ * work on rows and do not change; queries and keys may be normed per head; attention, norms and rotation are the operators above.
+ *
+ * Sequence i owns the rows offsets[i] .. offsets[i + 1] - 1 (int32 [nseq + 1] on the device, not falling) of the queries.  With
+ * 0 < T_q < T the first T - T_q rows of x are a prefix that every sequence sees in front of its own rows: keys and values
+ * of it are computed once, queries and y exist for the T_q rows behind it.  With shape->rope positions count within the
+ * sequence, from 0 or behind the prefix.  Rows that belong to no sequence take no part: their y and dx are 0, and the weights' gradients
+ * have nothing of them (their routing is computed like every row's).
+ */
+typedef struct {
+  int32_t nseq;                 /* >= 1                                                                              */
+  int32_t max_len;              /* no sequence is longer: further rows are treated as not there                      */
+  const int32_t* offsets;
+  const void *q_norm, *k_norm;  /* [d_head] in storage type: weights of the norms of queries and keys (x w /
+                                   sqrt(mean(x^2) + norm_eps), before the rotation); both NULL: no norms             */
+  float norm_eps;
+} sh_packing;
+
+/* Bytes of workspace of the two calls below; 0 if shape or packing are invalid.  Host-only (offsets may be NULL).
+ * get_routing and get_intermediates read such a workspace like a plain layer's (Q and K before their norms). */
+size_t switchhead_packed_workspace_bytes(const sh_shape* shape, const sh_packing* packing);
+
+/* As switchhead_forward; B must be 1. */
+sh_status switchhead_forward_packed(const sh_shape* shape, const sh_packing* packing,
+                                    const void* x, const void* W_Q, const void* W_K,
+                                    const void* W_V, const void* W_O,
+                                    const void* W_S, const void* W_D,
+                                    const float* b_S, const float* b_D,
+                                    void* y, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* As switchhead_backward, on the workspace of switchhead_forward_packed; dq_norm, dk_norm: fp32 [d_head] gradients of the norms'
+ * weights, or NULL.  No prefix (T_q must be 0 or T). */
+sh_status switchhead_backward_packed(const sh_shape* shape, const sh_packing* packing,
+                                     const void* x, const void* W_Q, const void* W_K,
+                                     const void* W_V, const void* W_O,
+                                     const void* W_S, const void* W_D,
+                                     const void* dy, void* workspace, size_t workspace_bytes,
+                                     void* dx, float* dW_Q, float* dW_K, float* dW_V, float* dW_O,
+                                     float* dW_S, float* dW_D, float* db_S, float* db_D,
+                                     float* dq_norm, float* dk_norm, void* hip_stream);
+
 /* Description of the last error on this thread ("" if none). Never NULL. */
 const char* switchhead_last_error(void);
 

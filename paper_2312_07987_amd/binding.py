@@ -22,7 +22,8 @@ EXPORTS = ("switchhead_workspace_bytes", "switchhead_workspace_parts", "switchhe
            "switchhead_set_kernel_family", "switchhead_version",
            "switchhead_profile_enable", "switchhead_profile_read",
            "switchhead_attention_workspace_bytes", "switchhead_attention_forward", "switchhead_attention_backward",
-           "switchhead_qk_norm_workspace_bytes", "switchhead_qk_norm_rope_forward", "switchhead_qk_norm_rope_backward")
+           "switchhead_qk_norm_workspace_bytes", "switchhead_qk_norm_rope_forward", "switchhead_qk_norm_rope_backward",
+           "switchhead_packed_workspace_bytes", "switchhead_forward_packed", "switchhead_backward_packed")
 
 
 class sh_shape(ctypes.Structure):
@@ -41,6 +42,11 @@ class sh_qk_norm(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int32) for n in ("tokens", "nheads", "nkv_heads", "d_head", "rope_dim", "dtype")] +
                 [("eps", ctypes.c_float), ("theta", ctypes.c_float)] +
                 [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "yq_row", "yq_head", "yk_row", "yk_head")])
+
+
+class sh_packing(ctypes.Structure):
+    _fields_ = [("nseq", ctypes.c_int32), ("max_len", ctypes.c_int32), ("offsets", ctypes.c_void_p), ("q_norm", ctypes.c_void_p),
+                ("k_norm", ctypes.c_void_p), ("norm_eps", ctypes.c_float)]
 
 
 class SwitchHeadError(RuntimeError):
@@ -103,6 +109,13 @@ def lib():
     L.switchhead_qk_norm_rope_forward.argtypes = [nrm] + [vp] * 7 + [vp]
     L.switchhead_qk_norm_rope_backward.restype = i32
     L.switchhead_qk_norm_rope_backward.argtypes = [nrm] + [vp] * 12 + [sz, vp]
+    pkg = ctypes.POINTER(sh_packing)
+    L.switchhead_packed_workspace_bytes.restype = sz
+    L.switchhead_packed_workspace_bytes.argtypes = [shp, pkg]
+    L.switchhead_forward_packed.restype = i32
+    L.switchhead_forward_packed.argtypes = [shp, pkg] + [vp] * 10 + [vp, sz, vp]
+    L.switchhead_backward_packed.restype = i32
+    L.switchhead_backward_packed.argtypes = [shp, pkg] + [vp] * 8 + [vp, sz] + [vp] * 11 + [vp]
     _lib = L
     return L
 
@@ -308,3 +321,26 @@ def switchhead_qk_norm_rope_backward(norm, Q, K, w_Q, w_K, positions, dY_Q, dY_K
     _launch(lib().switchhead_qk_norm_rope_backward, Q.device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
             _addr(dY_Q), _addr(dY_K), _addr(dQ), _addr(dK), _addr(dw_Q), _addr(dw_K),
             _addr(workspace), workspace.numel() * workspace.element_size())
+
+
+def make_packing(offsets, max_len, q_norm=None, k_norm=None, norm_eps=1e-6):
+    """Packed sequences of a layer call: offsets int32 [nseq + 1] on the GPU (kept alive by the packing), weights of the norms or None."""
+    p = sh_packing(offsets.numel() - 1, max_len, _addr(offsets), _addr(q_norm), _addr(k_norm), norm_eps)
+    p.tensors = (offsets, q_norm, k_norm)
+    return p
+
+
+def switchhead_packed_workspace_bytes(shape, packing):
+    return int(lib().switchhead_packed_workspace_bytes(shape, packing))
+
+
+def switchhead_forward_packed(shape, packing, x, W_Q, W_K, W_V, W_O, W_S, W_D, b_S, b_D, y, workspace, stream=None):
+    _launch(lib().switchhead_forward_packed, x.device, stream, shape, packing, _addr(x), _addr(W_Q), _addr(W_K), _addr(W_V), _addr(W_O),
+            _addr(W_S), _addr(W_D), _addr(b_S), _addr(b_D), _addr(y), _addr(workspace), workspace.numel() * workspace.element_size())
+
+
+def switchhead_backward_packed(shape, packing, x, W_Q, W_K, W_V, W_O, W_S, W_D, dy, workspace, dx, dW_Q, dW_K, dW_V, dW_O, dW_S, dW_D, db_S, db_D,
+                               dq_norm=None, dk_norm=None, stream=None):
+    _launch(lib().switchhead_backward_packed, x.device, stream, shape, packing, _addr(x), _addr(W_Q), _addr(W_K), _addr(W_V), _addr(W_O),
+            _addr(W_S), _addr(W_D), _addr(dy), _addr(workspace), workspace.numel() * workspace.element_size(), _addr(dx), _addr(dW_Q),
+            _addr(dW_K), _addr(dW_V), _addr(dW_O), _addr(dW_S), _addr(dW_D), _addr(db_S), _addr(db_D), _addr(dq_norm), _addr(dk_norm))

@@ -13,6 +13,7 @@
 
 #include "../../include/switchhead.h"
 #include "common.h"
+#include "packed_attn.h"
 
 using namespace sh;
 
@@ -173,7 +174,8 @@ bool list_shape(const sh_shape* s) {
   return s->dtype == SH_BF16 && s->d_model >= 256 && s->d_head >= 64 && s->nheads * s->E <= 64;
 }
 
-Layout make_layout(const sh_shape* s) {
+// (packed: sequences packed behind each other have an attention of their own, with its own workspace)
+Layout make_layout(const sh_shape* s, bool packed = false) {
   Layout L;
   const size_t N = (size_t)s->B * s->T, H = s->nheads, E = s->E, k = s->k, dh = s->d_head, dm = s->d_model;
   const size_t esz = s->dtype == SH_BF16 ? 2 : 4;
@@ -283,7 +285,7 @@ Layout make_layout(const sh_shape* s) {
   {
     int ld = 0;
     long per = 0;
-    if (s->dtype == SH_BF16 && attn_ds_dims(s->T, s->T_q, (int)dh, s->causal, &ld, &per)) {
+    if (!packed && s->dtype == SH_BF16 && attn_ds_dims(s->T, s->T_q, (int)dh, s->causal, &ld, &per)) {
       const size_t bytes = (size_t)s->B * H * (size_t)per * 2;
       // It lives from the dK / dV kernel to the dQ product.  The fp32 accumulator of dx (first written after the
       // attention backward) and the per-slot rows of the output experts' dgrad (consumed before it), which lie next to
@@ -334,6 +336,59 @@ Layout make_layout(const sh_shape* s) {
   return L;
 }
 
+// A layer over packed sequences (switchhead_forward_packed): what lies behind the layer's own workspace
+struct PackedLayer {
+  const sh_packing* p;
+  int prefix;                              // rows in front of the sequences that all of them see
+  bool norm;
+  sh_attention attention;
+  size_t pos, qn, kn, op, op_bytes, total; // positions [T]; normed queries and keys (norm only); workspace of the operators
+};
+
+sh_status packed_layout(PackedLayer& k, const sh_shape* s, const sh_packing* p) {
+  if (!p) return fail(SH_ERR_INVALID_ARG, "packing is NULL");
+  if (s->B != 1) return fail(SH_ERR_INVALID_ARG, "packed sequences need B = 1 (T rows in all), not B=%d", s->B);
+  const int Tq = s->T_q > 0 ? s->T_q : s->T;
+  if (p->nseq < 1 || p->max_len < 1) return fail(SH_ERR_INVALID_ARG, "nseq and max_len must be >= 1 (%d, %d)", p->nseq, p->max_len);
+  if ((p->q_norm == nullptr) != (p->k_norm == nullptr)) return fail(SH_ERR_INVALID_ARG, "q_norm and k_norm come together");
+  if (!(p->norm_eps >= 0.f) || !(p->norm_eps <= 3.0e38f)) return fail(SH_ERR_INVALID_ARG, "norm_eps must be finite and >= 0");
+  const size_t align = s->dtype == SH_BF16 ? 2 : 4;
+  if ((uintptr_t)p->q_norm % align || (uintptr_t)p->k_norm % align || (uintptr_t)p->offsets % 4) return fail(SH_ERR_INVALID_ARG, "offsets, q_norm or k_norm are not aligned to their elements");
+  k.p = p;
+  k.prefix = s->T - Tq;
+  k.norm = p->q_norm != nullptr;
+  sh_attention& a = k.attention;
+  a = sh_attention{};
+  a.nseq = p->nseq;
+  a.nheads = a.nkv_heads = s->nheads;
+  a.d_head = s->d_head;
+  a.causal = s->causal;
+  a.dtype = s->dtype;
+  a.total_q = a.total_k = Tq;
+  a.max_q = a.max_k = p->max_len;
+  a.prefix = k.prefix;
+  // (a backward pass takes no prefix)
+  k.op_bytes = switchhead_attention_workspace_bytes(&a, k.prefix == 0);
+  if (k.op_bytes == 0) return SH_ERR_UNSUPPORTED;   // (the text is set)
+  const size_t esz = s->dtype == SH_BF16 ? 2 : 4, rows = (size_t)s->T * s->nheads * s->d_head * esz;
+  size_t off = make_layout(s, true).total;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off += align_up(bytes);
+    return o;
+  };
+  k.pos = take((size_t)s->T * 4);
+  k.qn = k.norm ? take(rows) : 0;
+  k.kn = k.norm ? take(rows) : 0;
+  const size_t nb = packed_norm_bytes(s->T, s->nheads, s->d_head, s->dtype == SH_BF16);
+  if (nb > k.op_bytes) k.op_bytes = nb;
+  k.op = take(k.op_bytes);
+  // (not below the plain layer's, so that get_routing and get_intermediates take the workspace)
+  const size_t plain = make_layout(s).total;
+  k.total = off > plain ? off : plain;
+  return SH_OK;
+}
+
 struct Ctx {
   const sh_shape* s;
   Layout L;
@@ -343,6 +398,7 @@ struct Ctx {
   int Tq, Nq;   // queries per sequence and in all; Tq < T: only the last Tq positions are destinations
   bool rect;    // Tq < T
   bool dense, shared, qk_experts;
+  const PackedLayer* pk = nullptr;
   bool aligned = true;   // every tensor pointer of the call is 16-byte aligned (the matrix-core kernels need it)
   int n(int side) const { return side ? Nq : N; }   // tokens of the source (0) / destination (1) side
   template <typename T>
@@ -357,15 +413,16 @@ struct Ctx {
 };
 
 sh_status make_ctx(Ctx& c, const sh_shape* s, const void* W_S, const void* W_D, const void* ws, size_t ws_bytes,
-                   void* stream) {
+                   void* stream, const PackedLayer* pk = nullptr) {
   sh_status r = check_shape(s);
   if (r != SH_OK) return r;
   c.s = s;
-  c.L = make_layout(s);
+  c.L = make_layout(s, pk != nullptr);
+  c.pk = pk;
   if (!ws) return fail(SH_ERR_INVALID_ARG, "workspace is NULL");
   if (((uintptr_t)ws & 255) != 0) return fail(SH_ERR_INVALID_ARG, "workspace must be 256-byte aligned");
-  if (ws_bytes < c.L.total)
-    return fail(SH_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, c.L.total);
+  const size_t need = pk ? pk->total : c.L.total;
+  if (ws_bytes < need) return fail(SH_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", ws_bytes, need);
   c.ws = (char*)ws;
   c.st = (hipStream_t)stream;
   c.N = s->B * s->T;
@@ -463,6 +520,30 @@ void wgrad(const Ctx& c, WgradArgs a, bool deterministic = true, bool zero = tru
     return;
   }
   launch_simt_wgrad(a, c.bf16, c.st);
+}
+
+// Norms and rotation of one side of a packed layer (0 queries, 1 keys): queries and keys have token counts of their own, so each is a call with one side.
+// Rows that belong to no sequence have position 0.
+QkNormArgs packed_norm(const Ctx& c, int side) {
+  const PackedLayer& k = *c.pk;
+  QkNormArgs n{};
+  void* const x = c.p<void>(side ? c.L.K : c.L.Q);
+  void* const d = c.p<void>(side ? c.L.dK : c.L.dQ);
+  n.x[0] = x;
+  n.w[0] = side ? k.p->k_norm : k.p->q_norm;
+  n.norm = k.norm;
+  n.y[0] = k.norm ? c.p<void>(side ? k.kn : k.qn) : x;
+  n.dy[0] = n.dx[0] = d;
+  n.positions = c.p<int>(k.pos) + (side ? 0 : k.prefix);
+  n.tokens = side ? c.N : c.Nq;
+  n.H[0] = c.H;
+  n.dh = c.dh;
+  n.x_head[0] = n.y_head[0] = c.dh;
+  n.x_row[0] = n.y_row[0] = (long)c.H * c.dh;
+  n.rope_dim = c.s->rope ? c.dh / 2 * 2 : 0;
+  n.eps = k.p->norm_eps;
+  n.part = c.p<float>(k.op);
+  return n;
 }
 
 // rows taken through the expert-sorted permutation of one side
@@ -629,11 +710,11 @@ sh_status switchhead_workspace_parts(const sh_shape* shape, size_t* kept_bytes, 
   return SH_OK;
 }
 
-sh_status switchhead_forward(const sh_shape* shape, const void* x, const void* W_Q, const void* W_K, const void* W_V,
-                             const void* W_O, const void* W_S, const void* W_D, const float* b_S, const float* b_D,
-                             void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+static sh_status layer_forward(const sh_shape* shape, const PackedLayer* pk, const void* x, const void* W_Q, const void* W_K, const void* W_V,
+                               const void* W_O, const void* W_S, const void* W_D, const float* b_S, const float* b_D,
+                               void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
   Ctx c;
-  sh_status r = make_ctx(c, shape, W_S, W_D, workspace, workspace_bytes, hip_stream);
+  sh_status r = make_ctx(c, shape, W_S, W_D, workspace, workspace_bytes, hip_stream, pk);
   if (r != SH_OK) return r;
   if (!x || !W_Q || !W_K || !W_V || !W_O || !y) return fail(SH_ERR_INVALID_ARG, "x, W_Q, W_K, W_V, W_O, y must not be NULL");
   if (c.dense && W_D) return fail(SH_ERR_INVALID_ARG, "W_D given without W_S");
@@ -913,8 +994,15 @@ sh_status switchhead_forward(const sh_shape* shape, const void* x, const void* W
     }
   }
 
-  // rotary position embedding of queries and keys (App. A.4 "RoPE Positional Encodings")
-  if (shape->rope) {
+  // rotary position embedding of queries and keys (App. A.4 "RoPE Positional Encodings"); packed sequences: with the norms, where there are any
+  if (pk) {
+    if (pk->norm || shape->rope) {
+      prof_mark(c.st, "fwd.norm_rope");
+      if (shape->rope) launch_packed_positions(pk->p->offsets, pk->p->nseq, pk->p->max_len, shape->T, pk->prefix, c.p<int>(pk->pos), c.st);
+      launch_layer_norm_rope(packed_norm(c, 0), c.bf16, false, c.st);
+      launch_layer_norm_rope(packed_norm(c, 1), c.bf16, false, c.st);
+    }
+  } else if (shape->rope) {
     prof_mark(c.st, "fwd.rope");
     launch_rope_table(c.p<float2>(c.L.rope), shape->T, dh, c.st);
     if (c.rect) {   // query i of a sequence sits at position (T - T_q) + i
@@ -957,7 +1045,16 @@ sh_status switchhead_forward(const sh_shape* shape, const void* x, const void* W
   }
 
   // step 4: one attention matrix per head
-  {
+  if (pk) {
+    prof_mark(c.st, "fwd.clear");
+    launch_packed_clear(pk->p->offsets, pk->p->nseq, pk->p->max_len, c.Nq, H * dh * (c.bf16 ? 2 : 4), c.p<void>(c.L.ctx), nullptr, nullptr, c.st);
+    const size_t front = (size_t)pk->prefix * H * dh * (c.bf16 ? 2 : 4);   // the prefix' rows of K and V
+    char* const K = c.p<char>(pk->norm ? pk->kn : c.L.K);
+    char* const V = c.p<char>(c.L.V);
+    r = switchhead_attention_forward(&pk->attention, c.p<void>(pk->norm ? pk->qn : c.L.Q), K + front, V + front, pk->prefix ? K : nullptr, pk->prefix ? V : nullptr,
+                                     pk->p->offsets, nullptr, pk->p->offsets, nullptr, c.p<void>(c.L.ctx), c.p<float>(c.L.lse), c.p<void>(pk->op), pk->op_bytes, c.st);
+    if (r != SH_OK) return r;
+  } else {
     prof_mark(c.st, "fwd.attention");
     AttnArgs a{};
     a.Q = c.p<void>(c.L.Q);
@@ -1096,6 +1193,29 @@ sh_status switchhead_forward(const sh_shape* shape, const void* x, const void* W
   return check_launch("switchhead_forward");
 }
 
+sh_status switchhead_forward(const sh_shape* shape, const void* x, const void* W_Q, const void* W_K, const void* W_V,
+                             const void* W_O, const void* W_S, const void* W_D, const float* b_S, const float* b_D,
+                             void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return layer_forward(shape, nullptr, x, W_Q, W_K, W_V, W_O, W_S, W_D, b_S, b_D, y, workspace, workspace_bytes, hip_stream);
+}
+
+size_t switchhead_packed_workspace_bytes(const sh_shape* shape, const sh_packing* packing) {
+  PackedLayer k;
+  if (check_shape(shape) != SH_OK || packed_layout(k, shape, packing) != SH_OK) return 0;
+  return k.total;
+}
+
+sh_status switchhead_forward_packed(const sh_shape* shape, const sh_packing* packing, const void* x, const void* W_Q, const void* W_K,
+                                    const void* W_V, const void* W_O, const void* W_S, const void* W_D, const float* b_S,
+                                    const float* b_D, void* y, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  PackedLayer k;
+  sh_status r = check_shape(shape);
+  if (r == SH_OK) r = packed_layout(k, shape, packing);
+  if (r != SH_OK) return r;
+  if (!packing->offsets) return fail(SH_ERR_INVALID_ARG, "offsets must not be NULL");
+  return layer_forward(shape, &k, x, W_Q, W_K, W_V, W_O, W_S, W_D, b_S, b_D, y, workspace, workspace_bytes, hip_stream);
+}
+
 sh_status switchhead_forward_static(const sh_shape* shape, const void* x, const void* W_Q, const void* W_K,
                                     const void* W_V, const void* W_O, const void* W_S, const void* W_D, const float* b_S,
                                     const float* b_D, void* y, void* hip_stream) {
@@ -1127,12 +1247,12 @@ sh_status switchhead_forward_static(const sh_shape* shape, const void* x, const 
                             hip_stream);
 }
 
-sh_status switchhead_backward(const sh_shape* shape, const void* x, const void* W_Q, const void* W_K, const void* W_V,
+static sh_status layer_backward(const sh_shape* shape, const PackedLayer* pk, float* dq_norm, float* dk_norm, const void* x, const void* W_Q, const void* W_K, const void* W_V,
                               const void* W_O, const void* W_S, const void* W_D, const void* dy, void* workspace,
                               size_t workspace_bytes, void* dx, float* dW_Q, float* dW_K, float* dW_V, float* dW_O,
                               float* dW_S, float* dW_D, float* db_S, float* db_D, void* hip_stream) {
   Ctx c;
-  sh_status r = make_ctx(c, shape, W_S, W_D, workspace, workspace_bytes, hip_stream);
+  sh_status r = make_ctx(c, shape, W_S, W_D, workspace, workspace_bytes, hip_stream, pk);
   if (r != SH_OK) return r;
   if (!x || !W_Q || !W_K || !W_V || !W_O || !dy || !dx || !dW_Q || !dW_K || !dW_V || !dW_O)
     return fail(SH_ERR_INVALID_ARG, "x, W_Q, W_K, W_V, W_O, dy, dx, dW_Q, dW_K, dW_V, dW_O must not be NULL");
@@ -1380,7 +1500,14 @@ sh_status switchhead_backward(const sh_shape* shape, const void* x, const void* 
   }
 
   // attention
-  {
+  if (pk) {
+    prof_mark(c.st, "bwd.clear");
+    launch_packed_clear(pk->p->offsets, pk->p->nseq, pk->p->max_len, N, H * dh * (c.bf16 ? 2 : 4), c.p<void>(c.L.dQ), c.p<void>(c.L.dK), c.p<void>(c.L.dV), c.st);
+    r = switchhead_attention_backward(&pk->attention, c.p<void>(pk->norm ? pk->qn : c.L.Q), c.p<void>(pk->norm ? pk->kn : c.L.K), c.p<void>(c.L.V), c.p<void>(c.L.ctx),
+                                      c.p<void>(c.L.dctx), c.p<float>(c.L.lse), pk->p->offsets, nullptr, pk->p->offsets, nullptr, c.p<void>(c.L.dQ),
+                                      c.p<void>(c.L.dK), c.p<void>(c.L.dV), c.p<void>(pk->op), pk->op_bytes, c.st);
+    if (r != SH_OK) return r;
+  } else {
     AttnBwdArgs a{};
     a.Q = c.p<void>(c.L.Q);
     a.K = c.p<void>(c.L.K);
@@ -1411,7 +1538,16 @@ sh_status switchhead_backward(const sh_shape* shape, const void* x, const void* 
   }
 
   // back through the rotation of queries and keys: gradients take the opposite turn
-  if (shape->rope) {
+  if (pk) {
+    if (pk->norm || shape->rope) {
+      prof_mark(c.st, "bwd.norm_rope");
+      QkNormArgs q = packed_norm(c, 0), k_ = packed_norm(c, 1);
+      q.dw[0] = dq_norm;
+      k_.dw[0] = dk_norm;
+      launch_layer_norm_rope(q, c.bf16, true, c.st);
+      launch_layer_norm_rope(k_, c.bf16, true, c.st);
+    }
+  } else if (shape->rope) {
     prof_mark(c.st, "bwd.rope");
     if (c.rect) {
       launch_rope_apply(c.p<void>(c.L.dQ), nullptr, c.p<float2>(c.L.rope), c.Nq, c.Tq, shape->T - c.Tq, H, dh, 1, c.bf16, c.st);
@@ -2093,6 +2229,28 @@ sh_status switchhead_backward(const sh_shape* shape, const void* x, const void* 
   run_list();
   prof_mark(c.st, nullptr);
   return check_launch("switchhead_backward");
+}
+
+sh_status switchhead_backward(const sh_shape* shape, const void* x, const void* W_Q, const void* W_K, const void* W_V,
+                              const void* W_O, const void* W_S, const void* W_D, const void* dy, void* workspace,
+                              size_t workspace_bytes, void* dx, float* dW_Q, float* dW_K, float* dW_V, float* dW_O,
+                              float* dW_S, float* dW_D, float* db_S, float* db_D, void* hip_stream) {
+  return layer_backward(shape, nullptr, nullptr, nullptr, x, W_Q, W_K, W_V, W_O, W_S, W_D, dy, workspace, workspace_bytes, dx, dW_Q, dW_K, dW_V, dW_O, dW_S,
+                        dW_D, db_S, db_D, hip_stream);
+}
+
+sh_status switchhead_backward_packed(const sh_shape* shape, const sh_packing* packing, const void* x, const void* W_Q, const void* W_K,
+                                     const void* W_V, const void* W_O, const void* W_S, const void* W_D, const void* dy, void* workspace,
+                                     size_t workspace_bytes, void* dx, float* dW_Q, float* dW_K, float* dW_V, float* dW_O,
+                                     float* dW_S, float* dW_D, float* db_S, float* db_D, float* dq_norm, float* dk_norm, void* hip_stream) {
+  PackedLayer k;
+  sh_status r = check_shape(shape);
+  if (r == SH_OK) r = packed_layout(k, shape, packing);
+  if (r != SH_OK) return r;
+  if (!packing->offsets) return fail(SH_ERR_INVALID_ARG, "offsets must not be NULL");
+  if (k.prefix > 0) return fail(SH_ERR_UNSUPPORTED, "the backward pass takes no shared prefix (T_q=%d, T=%d)", shape->T_q, shape->T);
+  return layer_backward(shape, &k, dq_norm, dk_norm, x, W_Q, W_K, W_V, W_O, W_S, W_D, dy, workspace, workspace_bytes, dx, dW_Q, dW_K, dW_V, dW_O, dW_S, dW_D,
+                        db_S, db_D, hip_stream);
 }
 
 sh_status switchhead_get_routing(const sh_shape* shape, const void* workspace, size_t workspace_bytes,

@@ -294,6 +294,7 @@ QkNormArgs norm_args(const sh_qk_norm& a, const void* Q, const void* K, const vo
   n.dh = a.d_head;
   n.rope_dim = a.rope_dim;
   n.eps = a.eps;
+  n.norm = 1;
   for (int k = 0; k < 7; ++k) n.rate[k] = a.rope_dim ? pow((double)a.theta, -2.0 * (1 << k) / a.rope_dim) : 0.;
   return n;
 }

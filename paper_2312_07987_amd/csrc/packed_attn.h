@@ -363,6 +363,7 @@ struct QkNormArgs {
   float* part;             // [work-groups][dh]
   long tokens, x_row[2], x_head[2], y_row[2], y_head[2];   // gradients lie as their tensors do
   int H[2], dh, rope_dim, hchunk;
+  int norm;                // 0: rotation alone
   float eps;
   double rate[7];          // theta^(-2 2^k / rope_dim)
 };
@@ -371,6 +372,13 @@ struct QkNormGrid {
 };
 QkNormGrid qk_norm_grid(long tokens, int H0, int H1, int dh, int bf16);
 void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipStream_t s);
+// for the layer (one side, dense rows): rates and alignment are filled in
+void launch_layer_norm_rope(QkNormArgs a, int bf16, bool backward, hipStream_t s);
+size_t packed_norm_bytes(long tokens, int heads, int dh, int bf16);
+// pos[r] = r for the prefix' rows, prefix + the row's place in its sequence for the others, 0 for rows of no sequence
+void launch_packed_positions(const int* offsets, int nseq, int max_len, int T, int prefix, int* pos, hipStream_t s);
+// zeros in the rows that belong to no sequence of up to three tensors (NULL: none)
+void launch_packed_clear(const int* offsets, int nseq, int max_len, int rows, int row_bytes, void* p0, void* p1, void* p2, hipStream_t s);
 
 // launchers
 void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s);

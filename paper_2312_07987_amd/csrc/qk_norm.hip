@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_fwd_kernel(QkNormArgs a) {
       for (int i = 0; i < N; ++i) sum = fmaf(x.v[i], x.v[i], sum);
 #pragma unroll
       for (int k = 1; k < LR; k <<= 1) sum += __shfl_xor(sum, k, 64);
-      const float r = 1.f / sqrtf(fmaf(sum, inv_d, a.eps));
+      const float r = a.norm ? 1.f / sqrtf(fmaf(sum, inv_d, a.eps)) : 1.f;
       float y[N];
 #pragma unroll
       for (int j = 0; j < N / 2; ++j) {
@@ -165,6 +165,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormArgs a) {
       for (int j = 0; j < N / 2; ++j) {
         dn[2 * j] = dy.v[2 * j] * cs[j] + dy.v[2 * j + 1] * sn[j];
         dn[2 * j + 1] = dy.v[2 * j + 1] * cs[j] - dy.v[2 * j] * sn[j];
+      }
+      if (!a.norm) {   // uniform
+        store_piece<T, AL>(dx_, d, a.dh, dn);
+        continue;
       }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
@@ -281,6 +285,57 @@ void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipSt
       launch_norm_lr<float, 64>(a, align, grid, backward, s);
   }
   if (backward && (a.dw[0] || a.dw[1])) qk_norm_dw_kernel<<<dim3((a.dh + 7) / 8, 2), 256, 0, s>>>(a.part, g.x, g.yq, g.y - g.yq, a.dh, a.dw[0], a.dw[1]);
+}
+
+void launch_layer_norm_rope(QkNormArgs a, int bf16, bool backward, hipStream_t s) {
+  for (int k = 0; k < 7; ++k) a.rate[k] = a.rope_dim ? pow(10000., -2. * (1 << k) / a.rope_dim) : 0.;
+  if (a.rope_dim == 0) a.positions = nullptr;
+  const int esz = bf16 ? 2 : 4;
+  const unsigned long bits = (unsigned long)a.dh * esz | (unsigned long)(uintptr_t)a.w[0];   // (the workspace's rows begin at multiples of 256)
+  launch_qk_norm_rope(a, bf16, bits % 16 == 0 ? 16 : bf16 && bits % 8 == 0 ? 8 : esz, backward, s);
+}
+size_t packed_norm_bytes(long tokens, int heads, int dh, int bf16) {
+  const QkNormGrid g = qk_norm_grid(tokens, heads, 0, dh, bf16);
+  return (size_t)g.x * g.y * dh * 4;
+}
+
+// The place of row q in its sequence, -1 if it belongs to none
+__device__ __forceinline__ int place_in_sequence(const int* offsets, int nseq, int max_len, int q) {
+  int lo = 0, hi = nseq;   // the last sequence that begins at or before q
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (offsets[mid] <= q)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  const int beg = max(offsets[lo], 0);
+  return q >= beg && q < offsets[lo + 1] && q - beg < max_len ? q - beg : -1;
+}
+
+__global__ __launch_bounds__(256) void packed_positions_kernel(const int* offsets, int nseq, int max_len, int T, int prefix, int* pos) {
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= T) return;
+  const int at = row < prefix ? -1 : place_in_sequence(offsets, nseq, max_len, row - prefix);
+  pos[row] = row < prefix ? row : at < 0 ? 0 : prefix + at;
+}
+
+// zeros in the rows of up to three tensors that belong to no sequence: a wave per row
+__global__ __launch_bounds__(256) void packed_clear_kernel(const int* offsets, int nseq, int max_len, int rows, int shorts, unsigned short* p0, unsigned short* p1, unsigned short* p2) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= rows || place_in_sequence(offsets, nseq, max_len, row) >= 0) return;
+  for (int i = threadIdx.x & 63; i < shorts; i += 64) {
+    const long at = (long)row * shorts + i;
+    if (p0) p0[at] = 0;
+    if (p1) p1[at] = 0;
+    if (p2) p2[at] = 0;
+  }
+}
+void launch_packed_clear(const int* offsets, int nseq, int max_len, int rows, int row_bytes, void* p0, void* p1, void* p2, hipStream_t s) {
+  packed_clear_kernel<<<dim3((rows + 3) / 4), 256, 0, s>>>(offsets, nseq, max_len, rows, row_bytes / 2, (unsigned short*)p0, (unsigned short*)p1, (unsigned short*)p2);
+}
+void launch_packed_positions(const int* offsets, int nseq, int max_len, int T, int prefix, int* pos, hipStream_t s) {
+  packed_positions_kernel<<<dim3((T + 255) / 256), 256, 0, s>>>(offsets, nseq, max_len, T, prefix, pos);
 }
 
 }  // namespace sh

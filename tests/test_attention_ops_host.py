@@ -159,3 +159,47 @@ def test_binding_checks_of_tensors():
     for call in bad:
         with pytest.raises(b.SwitchHeadError):
             call()
+
+
+def shape(**over):
+    f = dict(B=1, T=100, d_model=64, nheads=2, d_head=32, E=4, k=2, causal=1, dtype="f32")
+    f.update(over)
+    return b.make_shape(**f)
+
+
+def packing(**over):
+    f = dict(nseq=3, max_len=50, offsets=P, q_norm=None, k_norm=None, norm_eps=1e-6)
+    f.update(over)
+    return b.sh_packing(*f.values())
+
+
+def packed_forward(s, p, ws=1 << 40, **over):
+    a = dict(x=P, W_Q=P, W_K=P, W_V=P, W_O=P, W_S=P, W_D=P, b_S=None, b_D=None, y=P, workspace=P)
+    a.update(over)
+    return lib().switchhead_forward_packed(ctypes.byref(s), ctypes.byref(p) if p else None, *a.values(), ws, None)
+
+
+def packed_backward(s, p, ws=1 << 40, **over):
+    a = dict(x=P, W_Q=P, W_K=P, W_V=P, W_O=P, W_S=P, W_D=P, dy=P, workspace=P)
+    a.update(over)
+    return lib().switchhead_backward_packed(ctypes.byref(s), ctypes.byref(p), *a.values(), ws, *[P] * 11, None)
+
+
+def test_packed_layer_refusals():
+    ok = shape(), packing()
+    need = b.switchhead_packed_workspace_bytes(*ok)
+    assert need >= b.switchhead_workspace_bytes(ok[0])
+    assert packed_forward(*ok, ws=need - 1) == packed_backward(*ok, ws=need - 1) == b.SH_ERR_WORKSPACE_TOO_SMALL
+    for s, p in ((shape(B=2), packing()), (shape(), packing(nseq=0)), (shape(), packing(max_len=0)), (shape(), packing(q_norm=P)), (shape(), packing(k_norm=P)),
+                 (shape(), packing(norm_eps=-1.0)), (shape(), packing(norm_eps=float("nan"))), (shape(), packing(q_norm=P + 2, k_norm=P)),
+                 (shape(), packing(offsets=P + 2)), (shape(T=0), packing())):
+        assert b.switchhead_packed_workspace_bytes(s, p) == 0 and b.switchhead_last_error()
+        assert packed_forward(s, p) == b.SH_ERR_INVALID_ARG and packed_backward(s, p) == b.SH_ERR_INVALID_ARG
+    assert packed_forward(shape(), None) == b.SH_ERR_INVALID_ARG
+    # sizes can be asked for before there are offsets
+    assert b.switchhead_packed_workspace_bytes(shape(), packing(offsets=None)) == need
+    assert packed_forward(shape(), packing(offsets=None)) == b.SH_ERR_INVALID_ARG
+    # a prefix: forward only
+    assert packed_backward(shape(T_q=60), packing()) == b.SH_ERR_UNSUPPORTED
+    for n in ("x", "W_Q", "W_O", "y", "workspace"):
+        assert packed_forward(*ok, **{n: None}) == b.SH_ERR_INVALID_ARG
