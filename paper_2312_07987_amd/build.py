@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libswitchhead.so")
 OBJ = os.path.join(os.path.dirname(HERE), "_build")
 SOURCES = ["host.hip", "routing.hip", "small.hip", "simt.hip", "mfma_gemm.hip", "mfma_pp.hip", "mfma_skinny.hip", "mfma_wgrad.hip", "mfma_attn.hip", "mfma_f32.hip",
-           "host_ops.hip", "packed_fwd.hip", "packed_few.hip", "packed_bwd.hip", "qk_norm.hip"]
+           "host_ops.hip", "packed_fwd.hip", "packed_few.hip", "packed_prefix.hip", "packed_bwd.hip", "qk_norm.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -115,7 +115,7 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   // A prefix: sequences whose rows fill half a tile or more walk it themselves, ahead of their own keys; shorter ones put the rows of all
   // sequences into common tiles over the prefix, and their own keys are a second part.
   if (a.prefix > 0) {
-    p.two_parts = rows < 64 * seqs && rows * G < (1l << 32);
+    p.two_parts = rows < 128 * seqs && rows * G < (1l << 32);
     if (!p.two_parts) p.few = false;
   }
   const int kt = (a.d_head <= 64 || (p.esz == 2 && a.d_head <= 128)) ? 64 : 32;
@@ -130,7 +130,9 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
     const long tiles = (rows / PACKED_BM + seqs) * a.nkv_heads;
     const long kts = ceil_div((long)(p.two_parts ? 0 : a.prefix) + a.max_k, kt);
     p.groups = a.d_head <= 128 && kts >= 8 && tiles < 1024 ? 2 : 1;
-    if (p.esz == 2 && a.d_head <= 128 && most >= 1024 && ceil_div(rows, PACKED_BM2) * a.nkv_heads >= 256) {
+    // 256-row tiles, one work-group per CU, where there are several rounds of them: 1024 of them 672 -> 630 us (a prompt of 8192 tokens, 32 heads over 8),
+    // but 516 of them 158 -> 166 (6600 tokens, 20 heads over 4), where the longest one is most of the launch
+    if (!p.two_parts && p.esz == 2 && a.d_head > 32 && a.d_head <= 128 && most >= 1024 && ceil_div(rows, PACKED_BM2) * a.nkv_heads >= 768) {
       p.groups = 4;
       p.levels = levels(most, rows, PACKED_BM2);
     }
@@ -141,7 +143,8 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   }
   if (p.two_parts) {
     const long tiles = ceil_div(rows, PACKED_BM) * a.nkv_heads, kts = ceil_div(a.prefix, kt);
-    long ns = 512 / (tiles > 0 ? tiles : 1);
+    // (256 work-groups beside those of the own keys; more parts cost more to join than they save)
+    long ns = 256 / (tiles > 0 ? tiles : 1);
     if (ns > kts / 2) ns = kts / 2;
     if (ns > 32) ns = 32;
     p.nflat = (int)(ns < 1 ? 1 : ns);
@@ -346,28 +349,29 @@ sh_status switchhead_attention_forward(const sh_attention* d, const void* Q, con
   a.pl = (float*)(ws + p.pl);
   a.nparts = p.nsplit + p.nflat;
   a.frows = s.max_q * p.G;
-  if (p.two_parts) {
-    prof_mark(st, "attention.prefix");
-    PackedAttn f = a;
-    f.flat = 1;
-    f.groups = 1;
-    f.nsplit = p.nflat;
-    launch_packed_fwd(f, bf16, align, st);
-  }
   if (p.few) {
-    prof_mark(st, "attention.few");
     a.chunk = p.chunk;
     if (p.chunk || p.two_parts) {
       a.fo = (float*)(ws + p.fo);
       a.fl = (float*)(ws + p.fl);
     }
+  }
+  PackedAttn t = a;   // in tiles: this launch's parts
+  t.nsplit = p.nsplit;
+  t.part0 = p.nflat;
+  t.own = p.two_parts;
+  if (p.two_parts) {
+    prof_mark(st, "attention.prefix");
+    PackedAttn f = a;
+    f.flat = 1;
+    f.nsplit = p.nflat;
+    t.groups = 1;
+    launch_packed_prefix(f, p.few ? a : t, p.few, bf16, align, st);
+  } else if (p.few) {
+    prof_mark(st, "attention.few");
     launch_packed_few(a, bf16, align, st);
   } else {
     prof_mark(st, "attention.tiles");
-    PackedAttn t = a;
-    t.nsplit = p.nsplit;
-    t.part0 = p.nflat;
-    t.own = p.two_parts;
     launch_packed_fwd(t, bf16, align, st);
   }
   if (a.nparts || a.fo) {

@@ -383,12 +383,13 @@ void launch_packed_clear(const int* offsets, int nseq, int max_len, int rows, in
 // launchers
 void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s);
 void launch_packed_few(const PackedAttn& a, int bf16, int align, hipStream_t s);
+void launch_packed_prefix(const PackedAttn& f, const PackedAttn& o, bool few, int bf16, int align, hipStream_t s);
 void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s);
 void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta, hipStream_t s);
 
 enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128, PACKED_QT = 64 };
 // head width that a work-group's tiles are laid out for
-static inline int packed_width(int dh) { return dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
+static inline int packed_width(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
 // slots of `rows` rows in tiles of bm over nseq sequences
 static inline long packed_slots(long rows, int bm, int nseq) { return rows / bm + nseq; }
 

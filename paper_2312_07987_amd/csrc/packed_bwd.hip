@@ -479,7 +479,7 @@ __global__ __launch_bounds__(512) void packed_dkv_join_kernel(PackedAttnBwd b) {
 template <int DH, int AL>
 __global__ __launch_bounds__(256, 2) void packed_dq_ds_kernel(PackedAttnBwd b) {
   const PackedAttn& a = b.f;
-  constexpr int KT = 64, LD = col_ld<bf16_t, DH>(), BM = PACKED_BM, LDD = col_ld<bf16_t, BM>(), NDB = DH / 32, NP = KT * BM / 8 / 256;
+  constexpr int KT = 128, LD = DH + 16, BM = PACKED_BM, LDD = BM + 16, NDB = DH / 32, NP = KT * BM / 8 / 256;
   constexpr bool SPLIT = NDB % 2 == 0;
   constexpr int NJ = SPLIT ? 2 : 1, ND = SPLIT ? NDB / 2 : NDB;
   __shared__ __attribute__((aligned(16))) unsigned short Ks[KT * LD], Ds[KT * LDD];
@@ -578,8 +578,6 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
   frag_t<T> qf[NKD], gf[NKD];
   const raw* Q = (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head;
   const raw* G = (const raw*)b.dO + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head;
-  mem_frags<T, AL, NKD, 16>(qf, Q, 8 * g, dh, row < rows);
-  mem_frags<T, AL, NKD, 16>(gf, G, 8 * g, dh, row < rows);
   const float lse2 = a.lse[(long)head * a.total_q + s.qbeg + tok] * 1.44269504088896340736f;
   const float del = b.delta[(long)head * a.total_q + s.qbeg + tok];
   f32x16 acc[NDB];
@@ -595,6 +593,8 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
     tk.load(K, a.k_row, kend, dh, tid);
     tv.load(V, a.v_row, kend, dh, tid);
   }
+  mem_frags<T, AL, NKD, 16>(qf, Q, 8 * g, dh, row < rows);
+  mem_frags<T, AL, NKD, 16>(gf, G, 8 * g, dh, row < rows);
   __builtin_amdgcn_s_waitcnt(0x0F70);
   for (int k0 = 0; k0 < kend; k0 += KT) {
     __syncthreads();
@@ -697,7 +697,9 @@ static void launch_bwd_t(const PackedAttnBwd& b, int align, float* delta, hipStr
     else if constexpr (sizeof(T) == 4)
       launch_delta<T, 64>(b, align, delta, s);
   }
-  if (a.dh <= 64)
+  if (a.dh <= 32)
+    launch_bwd<T, 32>(b, align, s);
+  else if (a.dh <= 64)
     launch_bwd<T, 64>(b, align, s);
   else if (a.dh <= 96)
     launch_bwd<T, 96>(b, align, s);

@@ -6,216 +6,16 @@
 // stands.  K and V tiles go through LDS once for all rows of the work-group.
 #include <type_traits>
 
-#include "packed_attn.h"
+#include "packed_bodies.h"
 
 namespace sh {
 
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-// One work-group: 128 rows of one (sequence, kv head), four waves of 32, key tiles of KT.  NG = 2: two such groups of waves take
-// alternate tiles of the same rows and merge their (o, m, l) through LDS at the end.  That halves the chain of a long row of tiles, which is what a
-// batch of few long and many short sequences waits for, and the group has the CU to itself, so its two buffers per group (one barrier per trip)
-// fit.  16384 packed tokens, longest 4096, 4 heads of 128: 127 us with one group, see the launch for what it is with two.
 template <typename T, int DH, int AL, int NG>
 __global__ __launch_bounds__(256 * NG, DH <= 128 && NG == 1 ? 2 : 1) void packed_fwd_kernel(PackedAttn a) {
-  typedef typename Elem<T>::raw raw;
-  constexpr int KT = DH * sizeof(T) > 256 ? 32 : 64, LDK = row_ld<T, DH>(), LDV = col_ld<T, DH>(), NKD = DH / 16, NDB = DH / 32, BM = PACKED_BM;
-  constexpr int NBUF = NG, TILE = KT * (LDK + LDV);
-  __shared__ __attribute__((aligned(16))) raw kv_[NG * NBUF * TILE];
-
-  int b = blockIdx.x;
-  const int hk = b % a.Hk;
-  b /= a.Hk;
-  const int ns = max(a.nsplit, 1), split = b % ns, slot = b / ns;
-  const int grp = NG > 1 ? threadIdx.x >> 8 : 0;
-  const int tid = threadIdx.x & 255, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
-  raw* const kv = kv_ + grp * NBUF * TILE;
-
-  SeqGeom s;
-  int row0;
-  if (a.flat) {
-    s.qbeg = 0;
-    s.lq = a.total_q;
-    s.kbeg = s.lk = 0;
-    row0 = slot * BM;
-  } else if (a.levels) {
-    s = seq_geom(a, level_seq(slot, a.nseq));
-    row0 = (a.levels - 1 - slot / a.nseq) * BM;
-  } else {
-    int nth;
-    if (!find_slot<false>(a, BM, slot, nth, s)) return;
-    // the last tiles, which see most keys, first
-    const int nt = (s.lq * a.G + BM - 1) / BM;
-    if (nth >= nt) return;
-    row0 = (nt - 1 - nth) * BM;
-  }
-  const int rows = s.lq * a.G;
-  if (row0 >= rows) return;
-  const int off = s.lk - s.lq;   // query i sees own keys <= off + i
-  const int row = row0 + wave * 32 + r;
-  const int tok = div_by(min(row, rows - 1), a.g_inv), head = hk * a.G + min(row, rows - 1) - tok * a.G;
-  const int qpos = tok + off;
-  const int wq_first = div_by(min(row0 + wave * 32, rows - 1), a.g_inv) + off;
-  const int wq_last = div_by(min(row0 + wave * 32 + 31, rows - 1), a.g_inv) + off;
-  const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv);
-  const int prefix = a.own ? 0 : a.prefix;
-  const int kend = a.flat ? 0 : max(0, a.causal ? min(s.lk, last_tok + off + 1) : s.lk);   // own keys that some row sees
-
-  frag_t<T> qf[NKD];
-  const raw* Q = (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head;
-  mem_frags<T, AL, NKD, 16>(qf, Q, 8 * g, dh, row < rows);
-
-  f32x16 o[NDB];
-#pragma unroll
-  for (int d = 0; d < NDB; ++d) o[d] = zero16();
-  float m = -INFINITY, l = 0.f;
-  const float sc = a.scale * 1.44269504088896340736f;   // logits in log2 units
-
-  // tiles of the prefix, then of the own keys; this work-group's even share of them
-  const int np = (prefix + KT - 1) / KT, nt = np + (kend + KT - 1) / KT;
-  const int t0 = (int)((unsigned)(nt * split) / (unsigned)ns), t1 = (int)((unsigned)(nt * (split + 1)) / (unsigned)ns);   // (below 2^25 tiles, 32 parts)
-  PieceTile<T, DH, AL, KT, 256> tk, tv;
-  const raw* const KP = (const raw*)a.KP + (long)hk * a.kp_head;
-  const raw* const VP = (const raw*)a.VP + (long)hk * a.vp_head;
-  const raw* const K = (const raw*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;
-  const raw* const V = (const raw*)a.V + (long)s.kbeg * a.v_row + (long)hk * a.v_head;
-  auto valid_of = [&](int t) { return t < np ? prefix - t * KT : kend - (t - np) * KT; };
-  // (the prefix may have other strides: the pieces are placed again at the border)
-  tk.place(t0 + grp < np ? a.kp_row : a.k_row, tid);
-  tv.place(t0 + grp < np ? a.vp_row : a.v_row, tid);
-  auto load = [&](int t) {
-    if (t >= np && t < np + NG) {
-      tk.place(a.k_row, tid);
-      tv.place(a.v_row, tid);
-    }
-    if (t < np) {
-      tk.load(KP + (long)t * KT * a.kp_row, a.kp_row, valid_of(t), dh, tid);
-      tv.load(VP + (long)t * KT * a.vp_row, a.vp_row, valid_of(t), dh, tid);
-    } else {
-      tk.load(K + (long)(t - np) * KT * a.k_row, a.k_row, valid_of(t), dh, tid);
-      tv.load(V + (long)(t - np) * KT * a.v_row, a.v_row, valid_of(t), dh, tid);
-    }
-  };
-  auto store = [&](int t, raw* buf) {
-    tk.store(buf, LDK, valid_of(t), dh, tid);
-    tv.store(buf + KT * LDK, LDV, valid_of(t), dh, tid);
-  };
-  if (t0 + grp < t1) load(t0 + grp);
-  __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): what was loaded before the loop is not waited for again inside it
-  if constexpr (NG == 2) {
-    if (t0 + grp < t1) store(t0 + grp, kv);
-    if (t0 + grp + 2 < t1) load(t0 + grp + 2);
-    __syncthreads();
-  }
-  // NG = 2, one barrier per trip: while a tile is multiplied out of one buffer the next one (requested a trip ago) is written into the other and
-  // the one after that starts to travel.  NG = 1: the tile in the registers is written between two barriers.  All waves make the same trips.
-  int cur = 0;
-  for (int tb = t0; tb < t1; tb += NG, cur ^= NBUF - 1) {
-    const int t = tb + grp, valid = valid_of(t), k0 = (t - np) * KT;
-    const raw *const Ks = kv + cur * TILE, *const Vs = Ks + KT * LDK;
-    if constexpr (NG == 2) {
-      if (t + 2 < t1) {
-        store(t + 2, kv + (cur ^ 1) * TILE);
-        if (t + 4 < t1) load(t + 4);
-      }
-    } else {
-      __syncthreads();
-      store(t, kv);
-      __syncthreads();
-      if (t + 1 < t1) load(t + 1);
-    }
-    const bool masked = a.causal && t >= np;
-    // wave-uniform: a tile past the end, no rows, or nothing that they see
-    if (t < t1 && row0 + wave * 32 < rows && !(masked && k0 > wq_last)) {
-      f32x16 sv[KT / 32];
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb) {
-        sv[kb] = zero16();
-#pragma unroll
-        for (int kk = 0; kk < NKD; ++kk) sv[kb] = mma32(row_frag(&Ks[(kb * 32 + r) * LDK + kk * 16 + 8 * g]), qf[kk], sv[kb]);
-      }
-      if (valid < KT || (masked && k0 + KT - 1 > wq_first)) {
-        const int lim = (masked ? min(valid - 1, qpos - k0) : valid - 1) - 4 * g;
-#pragma unroll
-        for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (kb * 32 + 8 * (i >> 2) + (i & 3) > lim) sv[kb][i] = -INFINITY;
-      }
-      float mt = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sv[kb][i]);
-      mt = fmaxf(mt, __shfl_xor(mt, 32, 64)) * sc;   // sc > 0
-      const float mn = fmaxf(m, mt);
-      if (__ballot(mn > m)) {   // most tiles move no maximum
-        const float alpha = mn > m ? __builtin_amdgcn_exp2f(m - mn) : 1.f;   // m = -inf: 0
-        l *= alpha;
-#pragma unroll
-        for (int d = 0; d < NDB; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
-      }
-      m = mn;
-      const float mb = mn == -INFINITY ? 0.f : mn;   // (a row that has seen no key yet)
-      float ps = 0.f;
-#pragma unroll
-      for (int kb = 0; kb < KT / 32; ++kb)
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          float p8[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            p8[i] = __builtin_amdgcn_exp2f(fmaf(sv[kb][8 * st + i], sc, -mb));   // masked: 0
-            ps += p8[i];
-          }
-          // P is rounded to the storage type for its product; the sum keeps 32 bits
-          frag_t<T> pb;
-          pack_frag(pb, p8);
-          const int kr = kb * 32 + 16 * st + 4 * g;
-#pragma unroll
-          for (int d = 0; d < NDB; ++d) o[d] = mma32(col_frag(Vs, LDV, kr, kr + 8, d * 32, lane), pb, o[d]);
-        }
-      l += ps;
-    }
-    if constexpr (NG == 2) __syncthreads();
-  }
-  l += __shfl_xor(l, 32, 64);
-  if constexpr (NG == 2) {
-    // group 1 parks its partial results over the tiles; group 0 of the same wave and lane holds the same row and elements
-    static_assert(4 * (NDB * 16 + 2) * 64 * 4 <= NG * NBUF * TILE * (int)sizeof(raw), "the parked accumulators fit over the tiles");
-    float* park = (float*)kv_ + wave * (NDB * 16 + 2) * 64 + lane;
-    if (grp == 1) {
-#pragma unroll
-      for (int d = 0; d < NDB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) park[(d * 16 + i) * 64] = o[d][i];
-      park[NDB * 16 * 64] = m;
-      park[(NDB * 16 + 1) * 64] = l;
-    }
-    __syncthreads();
-    if (grp == 1) return;
-    const float m1 = park[NDB * 16 * 64], l1 = park[(NDB * 16 + 1) * 64], mn = fmaxf(m, m1), mb = mn == -INFINITY ? 0.f : mn;
-    const float f0 = __builtin_amdgcn_exp2f(m - mb), f1 = __builtin_amdgcn_exp2f(m1 - mb);   // a group that saw no key: 0
-#pragma unroll
-    for (int d = 0; d < NDB; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[d][i] = o[d][i] * f0 + park[(d * 16 + i) * 64] * f1;
-    l = l * f0 + l1 * f1;
-    m = mn;
-  }
-  if (row >= rows) return;
-  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // nothing seen: zeros; NaN stays
-  const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
-  if (a.nsplit) {
-    const long at = (long)(a.part0 + split) * a.total_q * a.H + (long)(s.qbeg + tok) * a.H + head;
-    if (g == 0) a.pl[at] = lse;
-    store_row<float, 16, NDB>(a.po + at * a.dhp, o, inv, g, dh);
-  } else {
-    if (g == 0 && a.lse) a.lse[(long)head * a.total_q + s.qbeg + tok] = lse;
-    store_row<T, AL, NDB>((raw*)a.O + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head, o, inv, g, dh);
-  }
+  __shared__ __attribute__((aligned(16))) typename Elem<T>::raw kv[packed_fwd_lds<T, DH, NG>()];
+  packed_fwd_body<T, DH, AL, NG>(a, blockIdx.x, kv);
 }
 
 // the larger of the two lane halves' values, in both
@@ -269,7 +69,6 @@ __global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn 
     const int row = min(wr + j * 32 + r, rows - 1);
     tok[j] = div_by(row, a.g_inv);
     head[j] = hk * a.G + row - tok[j] * a.G;
-    mem_frags<bf16_t, AL, NKD, 16>(qf[j], (const raw*)a.Q + (long)(s.qbeg + tok[j]) * a.q_row + (long)head[j] * a.q_head, 8 * g, dh, wr + j * 32 + r < rows);
   }
   f32x16 o[NJ][NDB];
 #pragma unroll
@@ -324,6 +123,9 @@ __global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn 
     // tile t0 of both, tile t0 + 1 of K; zeros where the first step's products with P = 0 read V
     load_k(t0);
     load_v(t0);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)   // (behind the tile's loads: what is done with them waits for them)
+      mem_frags<bf16_t, AL, NKD, 16>(qf[j], (const raw*)a.Q + (long)(s.qbeg + tok[j]) * a.q_row + (long)head[j] * a.q_head, 8 * g, dh, wr + j * 32 + r < rows);
     for (int i = tid; i < TV / 8; i += NT) *(uint4*)(Vs + 2 * TV + i * 8) = make_uint4(0, 0, 0, 0);
     tk.store(Ks, LDK, valid_of(t0), dh, tid);
     tv.store(Vs, LDV, valid_of(t0), dh, tid);
@@ -492,7 +294,7 @@ __global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn 
 
 template <typename T, int DH, int AL>
 static void launch_fwd_al(const PackedAttn& a, dim3 grid, hipStream_t s) {
-  if constexpr (DH <= 128 && sizeof(T) == 2) {
+  if constexpr (DH >= 64 && DH <= 128 && sizeof(T) == 2) {
     if (a.groups == 4) {
       packed_fwd_long_kernel<DH, AL, 1, 8><<<grid, 512, 0, s>>>(a);
       return;
@@ -516,7 +318,9 @@ static void launch_fwd(const PackedAttn& a, int align, dim3 grid, hipStream_t s)
 }
 template <typename T>
 static void launch_fwd_t(const PackedAttn& a, int align, dim3 grid, hipStream_t s) {
-  if (a.dh <= 64)
+  if (a.dh <= 32)
+    launch_fwd<T, 32>(a, align, grid, s);
+  else if (a.dh <= 64)
     launch_fwd<T, 64>(a, align, grid, s);
   else if (a.dh <= 96)
     launch_fwd<T, 96>(a, align, grid, s);
