@@ -275,7 +275,8 @@ sh_status switchhead_get_intermediates(const sh_shape* shape,
  *
  * over the keys u that query i of its sequence sees: all rows of the prefix, and of its n_k own keys all, or with `causal` those
  * with u <= (n_k - n_q) + i (the last query sees every key).  A query that sees nothing has O = 0, lse = -infinity and gives
- * no gradient.  What lies in keys and values behind a sequence's length has no influence, NaN included.
+ * no gradient.  What lies in keys and values behind a sequence's length has no influence, NaN included; a NaN or an infinity in
+ * a value that only `causal` hides may reach a query all the same (0 x NaN in a product), and in a key its gradients.
  */
 typedef struct {
   int32_t nseq;

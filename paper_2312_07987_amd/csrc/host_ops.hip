@@ -63,10 +63,13 @@ struct AttnPlan {
   int G, esz;
   bool few, two_parts;        // few rows per sequence: packed_few.hip; the prefix as a part of its own, for the rows of all sequences together
   int chunk, nsplit, nflat;   // keys of a few-row work-group (0: all); key ranges of the own keys and of the prefix
-  int groups, levels, levels128, klevels;   // wave groups of a tile's work-group; levels of the row tiles and of the key tiles, 0: by slot
+  int groups, tall;           // wave groups of a tile's work-group; tiles of 256 rows
+  int levels, levels128, klevels;   // levels of the row tiles (the forward's, the backward's) and of the key tiles, 0: by slot
   int dhp;
   size_t po, pl, fo, fl, total;
 };
+
+constexpr double MAX_THREADS = 4294967296.;   // of a launch
 
 // (the sizes that 32-bit row arithmetic and 24-bit reciprocals cover)
 sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
@@ -104,7 +107,8 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   p.chunk = 0;
   p.nsplit = p.nflat = 0;
   p.groups = 1;
-  // levels where their grid is at most twice that of slots, or small
+  p.tall = 0;
+  // levels where their grid is at most twice that of slots, or small: 16 sequences of 512 tokens 25.3 us by slots, 19.4 by levels; 3 of 4096 104 and 84
   auto levels = [&](long most, long all, int tile) {
     const long n = ceil_div(most, tile);
     return a.causal && n * a.nseq <= 2 * packed_slots(all, tile, a.nseq) + 1024 / a.nkv_heads ? (int)n : 0;
@@ -112,38 +116,52 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   p.levels = p.levels128 = levels(most, rows, PACKED_BM);
   p.klevels = levels(a.max_k, a.total_k, PACKED_KB);
   const long seqs = a.nseq > 0 ? a.nseq : 1;
-  // A prefix: sequences whose rows fill half a tile or more walk it themselves, ahead of their own keys; shorter ones put the rows of all
-  // sequences into common tiles over the prefix, and their own keys are a second part.
+  // A prefix: either every sequence's tiles walk it ahead of their own keys, or the rows of all sequences go into common tiles over it and
+  // the own keys are a second part.  The second saves what the first wastes in tiles that rows of one sequence do not fill (a sequence's last tile is
+  // half full on average), times the prefix, and pays for writing and joining two fp32 parts per row, about as long as 900 keys of a tile.
+  // Alone / in common, us, 4 heads of 128: 2048 shared keys, 64 sequences of 30 rows 44.1 / 33.8, of 100 rows 51 / 80; 500 shared keys (32 heads over 8),
+  // 64 sequences of 64 rows 34 / 43, of 4 rows 155 / 47 (4096 shared).
   if (a.prefix > 0) {
-    p.two_parts = rows < 128 * seqs && rows * G < (1l << 32);
+    const double tiles = std::fmin(std::fmax((double)seqs, rows / 128. + 0.5 * seqs), (double)ceil_div(most, PACKED_BM) * seqs);
+    p.two_parts = (p.few || a.prefix * (128. * tiles - rows) > 900. * rows) && rows * G < (1l << 32) && 64. * a.total_q * a.nheads < MAX_THREADS;
     if (!p.two_parts) p.few = false;
   }
   const int kt = (a.d_head <= 64 || (p.esz == 2 && a.d_head <= 128)) ? 64 : 32;
   if (p.few) {
-    // Chunks that make some 1500 work-groups of the keys there are; where a sequence's keys are few, one work-group takes them all
+    // Chunks that make some 1500 work-groups of the keys there are, of 512 keys or more where that makes 512 of them; where a sequence's keys are few, one
+    // work-group takes them all.  Chunks of 256 / 512: a token of 8192 keys, 32 heads over 8 (128 work-groups of 512) 14.2 / 16.8 us; 8 tokens of 32768 keys, 8
+    // heads over 1 (512) 35.9 / 30.3.  Unsplit, 32 tokens of 2000 .. 32768 keys take 428 instead of 317, 64 of 4000 each 185 instead of 197.
     const long keys = (long)a.max_k * seqs < a.total_k ? (long)a.max_k * seqs : a.total_k;
+    const long least = keys * a.nkv_heads >= 512 * 512 ? 512 : 256;
     long chunk = ceil_div(keys * a.nkv_heads, 1536);
-    chunk = ceil_div(chunk < 256 ? 256 : chunk > 1024 ? 1024 : chunk, 128) * 128;
+    chunk = ceil_div(chunk < least ? least : chunk > 1024 ? 1024 : chunk, 128) * 128;
     if (a.max_k > 2 * chunk || (a.max_k > chunk && seqs * a.nkv_heads < 256)) p.chunk = (int)chunk;
   } else {
-    // Few tiles and many keys: several work-groups share a tile's keys
     const long tiles = (rows / PACKED_BM + seqs) * a.nkv_heads;
     const long kts = ceil_div((long)(p.two_parts ? 0 : a.prefix) + a.max_k, kt);
-    p.groups = a.d_head <= 128 && kts >= 8 && tiles < 1024 ? 2 : 1;
-    // 256-row tiles, one work-group per CU, where there are several rounds of them: 1024 of them 672 -> 630 us (a prompt of 8192 tokens, 32 heads over 8),
-    // but 516 of them 158 -> 166 (6600 tokens, 20 heads over 4), where the longest one is most of the launch
-    if (!p.two_parts && p.esz == 2 && a.d_head > 32 && a.d_head <= 128 && most >= 1024 && ceil_div(rows, PACKED_BM2) * a.nkv_heads >= 768) {
-      p.groups = 4;
+    // Two wave groups where there is less than one round of work-groups, and tiles of keys for both.  One / two: 4 sequences of 2048 tokens, 4 heads, 62 / 49 us
+    // (272 tiles); 64 of 512 tokens, 4 heads, 48 / 65 (1280).
+    p.groups = a.d_head <= 128 && kts >= 8 && tiles < 1024 && !p.two_parts ? 2 : 1;
+    // 256-row tiles, one work-group per CU, for long rows of keys and three rounds of work-groups or more: 8192 tokens, 32 heads over 8 (1024 tiles) 623 -> 596 us, 2
+    // of them, 16 heads 632 -> 603, 3 of 4096, 20 heads over 4 (960) 310 -> 302; but 16 of 2048, 8 heads (1024) 186 -> 198, and 8192 tokens, 20 heads over 4
+    // (640 tiles, whose last round is half empty) 404 -> 414.
+    if (!p.two_parts && p.esz == 2 && a.d_head > 96 && a.d_head <= 128 && (long)a.prefix + a.max_k >= 4096 && most >= 4096 &&
+        ceil_div(rows, PACKED_BM2) * a.nkv_heads >= 768) {
+      p.tall = 1;
+      p.groups = 1;
       p.levels = levels(most, rows, PACKED_BM2);
     }
+    // Few tiles and many keys: several work-groups share a tile's keys, some 512 in all (256 of two wave groups) with 8 tiles of keys each or more.  17 queries over 8000 keys, 4
+    // heads, 141 us unsplit, 23 split; 512, 300, 64 over 2500, 300, 4000 77 and 28 (36 with half as many parts).
     long ns = 512 / p.groups / tiles;
     if (ns > kts / 8) ns = kts / 8;
     if (ns > 32) ns = 32;
-    p.nsplit = ns >= 2 || p.two_parts ? (int)(ns > 0 ? ns : 1) : 0;
+    p.nsplit = !p.tall && (ns >= 2 || p.two_parts) ? (int)(ns > 0 ? ns : 1) : 0;
   }
   if (p.two_parts) {
     const long tiles = ceil_div(rows, PACKED_BM) * a.nkv_heads, kts = ceil_div(a.prefix, kt);
-    // (256 work-groups beside those of the own keys; more parts cost more to join than they save)
+    // Some 256 work-groups beside those of the own keys; more parts cost more to join than they save: 64 tokens behind 4096 shared keys, 32 heads over 8, 29 us with 256,
+    // 38 with 512; 64 times 4 behind 8192 78 and 71, 131 with 128.
     long ns = 256 / (tiles > 0 ? tiles : 1);
     if (ns > kts / 2) ns = kts / 2;
     if (ns > 32) ns = 32;
@@ -165,6 +183,12 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
     p.fl = take(slots * 4);
   }
   p.total = off > 256 ? off : 256;
+  // (a launch has less than 2^32 threads)
+  const long nqs = p.levels ? (long)p.levels * a.nseq : packed_slots(rows, p.tall ? PACKED_BM2 : PACKED_BM, a.nseq);
+  const double own = p.few ? 256. * (p.chunk ? packed_slots(a.total_k, p.chunk, a.nseq) : a.nseq) : (p.tall || p.groups == 2 ? 512. : 256.) * nqs * (p.nsplit > 0 ? p.nsplit : 1);
+  const double flat = p.two_parts ? 256. * ceil_div(rows, PACKED_BM) * p.nflat : 0.;
+  if ((own + flat) * a.nkv_heads >= MAX_THREADS || ((p.nsplit || p.nflat || p.chunk) && 64. * a.total_q * a.nheads >= MAX_THREADS))
+    return fail(SH_ERR_UNSUPPORTED, "too large: the work-groups of nseq=%d, total_q=%d, total_k=%d, nheads=%d do not fit one launch", a.nseq, a.total_q, a.total_k, a.nheads);
   return SH_OK;
 }
 
@@ -173,6 +197,7 @@ struct BwdPlan {
   size_t dkv, ds, total;   // ds 0: not kept
   int rchunk, rparts;
   long ds_ld, dkv_floats;
+  double blocks;           // of its largest launch
 };
 constexpr size_t MAX_DS_BYTES = (size_t)2 << 30;
 BwdPlan plan_backward(const AttnPlan& p) {
@@ -207,6 +232,9 @@ BwdPlan plan_backward(const AttnPlan& p) {
       off += align_up(ds);
     }
   }
+  const double kb = p.klevels ? (double)p.klevels * a.nseq : packed_slots(a.total_k, PACKED_KB, a.nseq);
+  const double qb = p.levels128 ? (double)p.levels128 * a.nseq : packed_slots((long)a.total_q * p.G, PACKED_BM, a.nseq);
+  b.blocks = std::fmax(kb * b.rparts, std::fmax((double)packed_slots(a.total_k, PACKED_KB, a.nseq), qb)) * a.nkv_heads;
   b.total = off;
   return b;
 }
@@ -252,6 +280,7 @@ PackedAttn packed_args(const AttnPlan& p, const int32_t* qoff, const int32_t* ql
   a.scale = d.scale;
   a.dhp = p.dhp;
   a.groups = p.groups;
+  a.tall = p.tall;
   a.levels = p.levels;
   return a;
 }
@@ -365,7 +394,6 @@ sh_status switchhead_attention_forward(const sh_attention* d, const void* Q, con
     PackedAttn f = a;
     f.flat = 1;
     f.nsplit = p.nflat;
-    t.groups = 1;
     launch_packed_prefix(f, p.few ? a : t, p.few, bf16, align, st);
   } else if (p.few) {
     prof_mark(st, "attention.few");
@@ -398,6 +426,8 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
       !disjoint(s.total_k, s.nkv_heads, s.v_row, s.v_head, s.d_head))
     return fail(SH_ERR_INVALID_ARG, "the strides of Q, K or V lay the rows of a gradient over each other");
   const BwdPlan w = plan_backward(p);
+  if (512. * w.blocks >= MAX_THREADS)
+    return fail(SH_ERR_UNSUPPORTED, "too large: the work-groups of nseq=%d, total_q=%d, total_k=%d do not fit one launch", s.nseq, s.total_q, s.total_k);
   if ((r = check_workspace(workspace, workspace_bytes, w.total)) != SH_OK) return r;
   if (s.nseq == 0 || (s.total_q == 0 && s.total_k == 0)) return SH_OK;
   const hipStream_t st = (hipStream_t)hip_stream;

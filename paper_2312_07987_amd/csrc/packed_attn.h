@@ -39,7 +39,7 @@ struct PackedAttn {
   // `dense` parts [part][total_q * H] and, from the few-row kernel, [slot * Hk + kv head][frows].
   int nsplit, part0;                   // this launch's parts of the keys, the first one's number; nsplit 0: O is written
   int levels;                          // tiles of the longest sequence: work-groups numbered by level; 0: by slot
-  int groups;                          // 1, 2: wave groups of a work-group of 128 rows; 4: 256 rows (packed_fwd.hip)
+  int groups, tall;                    // wave groups of a work-group of 128 rows, 1 or 2; tall: 256 rows (packed_fwd.hip)
   int flat, own;                       // flat: rows of all tokens over the prefix alone; own: the sequence's own keys alone
   float *po, *pl;
   int dhp;                             // part row length: dh rounded up to 4
@@ -54,7 +54,7 @@ struct PackedAttnBwd {
   const void* dO;
   const float* delta;                  // [H][total_q]
   void *dQ, *dK, *dV;
-  // bf16, head widths 33 .. 128: score gradients dS^T [kv head][key][row of the sequence], rows of ds_ld, or NULL: computed again for dQ
+  // bf16, head widths up to 128: score gradients dS^T [kv head][key][row of the sequence], rows of ds_ld, or NULL: computed again for dQ
   void* dS;
   long ds_ld;
   // rows of a dK / dV work-group (a multiple of PACKED_QT): key tiles that see more leave fp32 parts, [part][slot * Hk + kv head][dV, dK] of

@@ -18,7 +18,9 @@ constexpr int packed_few_lds() {
 // One work-group: 128 rows of one (sequence, kv head), four waves of 32, key tiles of KT.  NG = 2: two such groups of waves take
 // alternate tiles of the same rows and merge their (o, m, l) through LDS at the end.  That halves the chain of a long row of tiles, which is what a
 // batch of few long and many short sequences waits for, and the group has the CU to itself, so its two buffers per group (one barrier per trip)
-// fit.  16384 packed tokens, longest 4096, 4 heads of 128: 127 us with one group, see the launch for what it is with two.
+// fit.  3 sequences of 4096 tokens, 4 heads of 128: 117 us with one group, 84 with two.
+// Bound by the chain of a tile of keys, products, softmax, products, where few waves share a SIMD (64 x 512 tokens, 8 heads of 128, 80 us: 430 TFLOP/s), by the
+// longest tile of rows where lengths differ.
 template <typename T, int DH, int AL, int NG>
 __device__ __forceinline__ void packed_fwd_body(const PackedAttn& a, int b, typename Elem<T>::raw* kv_) {
   typedef typename Elem<T>::raw raw;

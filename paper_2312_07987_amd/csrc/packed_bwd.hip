@@ -178,7 +178,7 @@ __device__ __forceinline__ bool key_tile(const PackedAttnBwd& b, int id, int& nt
   return nth >= 0;
 }
 
-// The same for bf16 heads of 33 .. 128 elements with two kinds of waves.  A single wave per SIMD, which is all that the kernel above has registers
+// The same for bf16 heads of up to 128 elements with two kinds of waves.  A single wave per SIMD, which is all that the kernel above has registers
 // for, leaves the matrix cores idle during exponentials, conversions and LDS traffic.  Here waves 0 .. 3 (score) hold the K and V fragments
 // of 32 keys each, form P and dS of a tile of 64 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
 // 4 .. 7 (gradient) hold the dK and dV accumulators, add the previous tile's products, and move the row tiles from memory to LDS.  One of each

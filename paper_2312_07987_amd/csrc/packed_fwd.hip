@@ -10,8 +10,6 @@
 
 namespace sh {
 
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
 template <typename T, int DH, int AL, int NG>
 __global__ __launch_bounds__(256 * NG, DH <= 128 && NG == 1 ? 2 : 1) void packed_fwd_kernel(PackedAttn a) {
   __shared__ __attribute__((aligned(16))) typename Elem<T>::raw kv[packed_fwd_lds<T, DH, NG>()];
@@ -24,26 +22,25 @@ __device__ __forceinline__ float half_max(float x) {
   return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
 }
 // ---------------------------------------------------------------------------------------------------------------------------
-// The same for bf16 and long rows of tiles: 4 waves x 64 rows, one wave per SIMD with all of its registers.
+// The same for bf16, heads of 97 .. 128 elements and long rows of keys: 256 rows, eight waves of 32, one work-group per CU.
 //
-// What bounds the kernel above is that its waves read every K and V fragment for 32 rows only (the LDS pipe is then as busy as the matrix cores)
-// and do one thing at a time: products, then the softmax, then products, with LDS latency in front of each.  Here a fragment serves 64 rows, and the
-// loop is a pipeline over steps of 32 keys whose three parts do not depend on each other: in step s the products S(s + 1) = K Q^T, the softmax of S(s)
-// and the products O += V^T P(s - 1)^T, 32 matrix instructions (1024 cycles) beside the vector instructions of 32 exponentials a lane (about
-// 800), interleaved by the scheduling groups.  K and V tiles of 64 keys lie in three LDS stages each: one barrier per tile.
+// A wave of the kernel above does one thing at a time, products, softmax, products, and counts on the other wave of its SIMD to fill the matrix cores
+// meanwhile.  Here the loop is a pipeline over steps of 32 keys whose three parts do not depend on each other: in step s the products
+// S(s + 1) = K Q^T, the softmax of S(s) and the products O += V^T P(s - 1)^T, 16 matrix instructions (512 cycles) with the vector instructions of 16
+// exponentials a lane issued between them.  K and V tiles of 64 keys, read once for 256 rows, lie in three LDS stages each: one barrier per tile.
 // The running maximum moves only where a tile's exceeds it by more than 2^8 in the exponent's base (P then stays below 2^8, which costs bf16
 // nothing), so the accumulators are hardly ever scaled.
+// Bound by what the vector and LDS pipes take between the products: 8192 tokens, 32 heads over 8 600 us, 916 TFLOP/s; with the matrix instructions alone
+// 433, without staging the tiles 550, without the exponentials 625 of 690 on the card where these were timed.  (64 rows a wave, one wave per SIMD, is no
+// help: a lone wave issues vector instructions at half rate.)  Narrower heads have fewer products to hide the same softmax behind: of 64, 4 x 2048
+// tokens, 128 us against 101 with the kernel above.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <int DH, int AL, int NJ, int NW>
-__global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn a) {
+template <int AL>
+__global__ __launch_bounds__(512, 1) void packed_fwd_long_kernel(PackedAttn a) {
   typedef unsigned short raw;
-  constexpr int KT = 64, LDK = row_ld<bf16_t, DH>(), LDV = col_ld<bf16_t, DH>(), NKD = DH / 16, NDB = DH / 32, BM = NW * 32 * NJ, NT = 64 * NW, TK = KT * LDK, TV = KT * LDV;
-  constexpr bool ACC = NW == 4;   // one wave per SIMD: 256 more registers that only matrix instructions and moves reach
+  constexpr int DH = 128, KT = 64, LDK = row_ld<bf16_t, DH>(), LDV = col_ld<bf16_t, DH>(), NKD = DH / 16, NDB = DH / 32, BM = PACKED_BM2, NT = 512, TK = KT * LDK, TV = KT * LDV;
   __shared__ __attribute__((aligned(16))) raw Ks[3 * TK], Vs[3 * TV];
-  int b = blockIdx.x;
-  const int hk = b % a.Hk;
-  b /= a.Hk;
-  const int ns = max(a.nsplit, 1), split = b % ns, slot = b / ns;
+  const int hk = blockIdx.x % a.Hk, slot = blockIdx.x / a.Hk;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = lane & 31, g = lane >> 5, dh = a.dh;
   SeqGeom s;
   int row0;
@@ -57,45 +54,31 @@ __global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn 
   }
   const int rows = s.lq * a.G;
   if (row0 < 0 || row0 >= rows) return;
-  const int off = s.lk - s.lq, wr = row0 + wave * 32 * NJ;
-  const int wq_first = div_by(min(wr, rows - 1), a.g_inv) + off, wq_last = div_by(min(wr + 32 * NJ - 1, rows - 1), a.g_inv) + off;
+  const int off = s.lk - s.lq, wr = row0 + wave * 32, row = wr + r;
+  const int wq_first = div_by(min(wr, rows - 1), a.g_inv) + off, wq_last = div_by(min(wr + 31, rows - 1), a.g_inv) + off;
   const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv);
-  const int prefix = a.own ? 0 : a.prefix;
+  const int prefix = a.prefix;
   const int kend = max(0, a.causal ? min(s.lk, last_tok + off + 1) : s.lk);
-  int tok[NJ], head[NJ];
-  bf16x8 qf[NJ][NKD];
+  const int tok = div_by(min(row, rows - 1), a.g_inv), head = hk * a.G + min(row, rows - 1) - tok * a.G;
+  bf16x8 qf[NKD];
+  f32x16 o[NDB];
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    const int row = min(wr + j * 32 + r, rows - 1);
-    tok[j] = div_by(row, a.g_inv);
-    head[j] = hk * a.G + row - tok[j] * a.G;
-  }
-  f32x16 o[NJ][NDB];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int d = 0; d < NDB; ++d) o[j][d] = zero16();
-  float m[NJ], l[NJ];
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    m[j] = -INFINITY;
-    l[j] = 0.f;
-  }
+  for (int d = 0; d < NDB; ++d) o[d] = zero16();
+  float m = -INFINITY, l = 0.f;
   const float sc = a.scale * 1.44269504088896340736f;
 
   const int np = (prefix + KT - 1) / KT, nt = np + (kend + KT - 1) / KT;
-  const int t0 = (int)((unsigned)(nt * split) / (unsigned)ns), t1 = (int)((unsigned)(nt * (split + 1)) / (unsigned)ns);
   // this wave's tiles: up to the last one with a key that one of its rows sees
   const int seen = !a.causal ? nt : np + (wq_last >= 0 ? wq_last / KT + 1 : 0);
-  const int tend = wr < rows ? min(t1, seen) : 0;
+  const int tend = wr < rows ? min(nt, seen) : 0;
   PieceTile<bf16_t, DH, AL, KT, NT> tk, tv;
   const raw* const KP = (const raw*)a.KP + (long)hk * a.kp_head;
   const raw* const VP = (const raw*)a.VP + (long)hk * a.vp_head;
   const raw* const K = (const raw*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;
   const raw* const V = (const raw*)a.V + (long)s.kbeg * a.v_row + (long)hk * a.v_head;
   auto valid_of = [&](int t) { return t < np ? prefix - t * KT : kend - (t - np) * KT; };
-  tk.place(t0 < np ? a.kp_row : a.k_row, tid);   // (the prefix may have other strides: placed again at the border)
-  tv.place(t0 < np ? a.vp_row : a.v_row, tid);
+  tk.place(0 < np ? a.kp_row : a.k_row, tid);   // (the prefix may have other strides: placed again at the border)
+  tv.place(0 < np ? a.vp_row : a.v_row, tid);
   auto load_k = [&](int t) {
     const bool p = t < np;
     if (t == np) tk.place(a.k_row, tid);
@@ -106,197 +89,144 @@ __global__ __launch_bounds__(64 * NW, 1) void packed_fwd_long_kernel(PackedAttn 
     if (t == np) tv.place(a.v_row, tid);
     tv.load((p ? VP : V) + (long)(p ? t : t - np) * KT * (p ? a.vp_row : a.v_row), p ? a.vp_row : a.v_row, valid_of(t), dh, tid);
   };
-  auto stage = [&](int t) { return (t - t0) % 3; };
-  auto hold = [](auto& tile) {   // a tile on its way waits in the accumulation registers
-#pragma unroll
-    for (int i = 0; i < tile.NCH; ++i)
-      if constexpr (ACC) asm volatile("" : "+a"(*(u32x4*)&tile.r[i]));
-  };
-  f32x16 S[2][NJ];   // [step parity][row block]
-  bf16x8 P[2][NJ][2];   // [step parity][row block][16 keys]
-#pragma unroll
-  for (int j = 0; j < NJ; ++j)
-#pragma unroll
-    for (int st = 0; st < 2; ++st) P[1][j][st] = bf16x8{};
+  f32x16 S[2];      // [step parity]
+  bf16x8 P[2][2];   // [step parity][16 keys]
+  P[1][0] = P[1][1] = bf16x8{};
 
-  if (t0 < t1) {
-    // tile t0 of both, tile t0 + 1 of K; zeros where the first step's products with P = 0 read V
-    load_k(t0);
-    load_v(t0);
-#pragma unroll
-    for (int j = 0; j < NJ; ++j)   // (behind the tile's loads: what is done with them waits for them)
-      mem_frags<bf16_t, AL, NKD, 16>(qf[j], (const raw*)a.Q + (long)(s.qbeg + tok[j]) * a.q_row + (long)head[j] * a.q_head, 8 * g, dh, wr + j * 32 + r < rows);
+  if (nt > 0) {
+    // tile 0 of both, tile 1 of K; zeros where the first step's products with P = 0 read V
+    load_k(0);
+    load_v(0);
+    // (behind the tile's loads: what is done with them waits for them)
+    mem_frags<bf16_t, AL, NKD, 16>(qf, (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head, 8 * g, dh, row < rows);
     for (int i = tid; i < TV / 8; i += NT) *(uint4*)(Vs + 2 * TV + i * 8) = make_uint4(0, 0, 0, 0);
-    tk.store(Ks, LDK, valid_of(t0), dh, tid);
-    tv.store(Vs, LDV, valid_of(t0), dh, tid);
-    if (t0 + 1 < t1) {
-      load_k(t0 + 1);
-      load_v(t0 + 1);
-      tk.store(Ks + TK, LDK, valid_of(t0 + 1), dh, tid);
+    tk.store(Ks, LDK, valid_of(0), dh, tid);
+    tv.store(Vs, LDV, valid_of(0), dh, tid);
+    if (nt > 1) {
+      load_k(1);
+      load_v(1);
+      tk.store(Ks + TK, LDK, valid_of(1), dh, tid);
     }
-    if (t0 + 2 < t1) load_k(t0 + 2);
+    if (nt > 2) load_k(2);
     __syncthreads();
+    S[0] = zero16();
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) S[0][j] = zero16();
-#pragma unroll
-    for (int kk = 0; kk < NKD; ++kk) {
-      const bf16x8 kf = row_frag(&Ks[r * LDK + kk * 16 + 8 * g]);
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) S[0][j] = mma32(kf, qf[j][kk], S[0][j]);
-    }
+    for (int kk = 0; kk < NKD; ++kk) S[0] = mma32(row_frag(&Ks[r * LDK + kk * 16 + 8 * g]), qf[kk], S[0]);
   }
-  // one step: PAR its parity; Kn the next step's 32 keys, Vp the previous step's.  The matrix instructions come in slots of two (the row blocks)
-  // that share a fragment, read three slots ahead; a slot's share of the softmax is issued behind them.  First the maximum, over the first SM
-  // slots, then the exponentials.
-  constexpr int NF = NKD + 2 * NDB, NS = NJ * NF, SM = NS / 4, AHEAD = 3;
+  // one step: PAR its parity; Kn the next step's 32 keys, Vp the previous step's.  The matrix instructions' fragments are read AHEAD ones before them, and a
+  // share of the softmax is issued behind each: first the maximum, over the first SM instructions, then the exponentials.
+  constexpr int NF = NKD + 2 * NDB, SM = NF / 4, AHEAD = 3;
   auto step = [&](int st_, auto par, const raw* Kn, const raw* Vp) {
     constexpr int PAR = decltype(par)::value;
     const int t = st_ >> 1, valid = valid_of(t) - 32 * PAR, k0 = (t - np) * KT + 32 * PAR;
     const bool masked = a.causal && t >= np;
-    // the products leave S in accumulation registers; Q and O stay there, which leaves the others to the softmax
-    f32x16 sv[NJ];
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      sv[j] = S[PAR][j];
-      if constexpr (ACC) {
-        asm volatile("" : "+v"(sv[j]));
-#pragma unroll
-        for (int kk = 0; kk < NKD; ++kk) asm volatile("" : "+a"(qf[j][kk]));
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) asm volatile("" : "+a"(o[j][d]));
-      }
-    }
+    f32x16 sv = S[PAR];
     if (valid < 32 || (masked && k0 + 31 > wq_first)) {   // wave-uniform
+      const int lim = (masked ? min(valid - 1, tok + off - k0) : valid - 1) - 4 * g;
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int lim = (masked ? min(valid - 1, tok[j] + off - k0) : valid - 1) - 4 * g;
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (8 * (i >> 2) + (i & 3) > lim) sv[j][i] = -INFINITY;
-      }
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i >> 2) + (i & 3) > lim) sv[i] = -INFINITY;
     }
     auto fragment = [&](int q) {
       const int i = q / 2;   // in turn: the score products are one chain, each waits for the one before it
       return q % 2 == 0 ? row_frag(&Kn[r * LDK + i * 16 + 8 * g]) : col_frag(Vp, LDV, 16 * (i / NDB) + 4 * g, 16 * (i / NDB) + 4 * g + 8, i % NDB * 32, lane);
     };
     bf16x8 f[NF];
-    float mt[NJ], mb[NJ], alpha[NJ], ps[NJ], p[NJ][16];
-    bool any = false;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) ps[j] = 0.f;
+    float mt, mb, alpha, ps = 0.f, p[16];
+    bool moved = false;
 #pragma unroll
     for (int q = 0; q < AHEAD; ++q) f[q] = fragment(q);
 #pragma unroll
-    for (int u = 0; u < NS; ++u) {
-      const int q = u / NJ, h = u % NJ;
-      if (h == 0 && q + AHEAD < NF) f[q + AHEAD] = fragment(q + AHEAD);
+    for (int q = 0; q < NF; ++q) {
+      if (q + AHEAD < NF) f[q + AHEAD] = fragment(q + AHEAD);
       const int i = q / 2;
       if (q % 2 == 0)
-        S[PAR ^ 1][h] = mma32(f[q], qf[h][i], i == 0 ? zero16() : S[PAR ^ 1][h]);
+        S[PAR ^ 1] = mma32(f[q], qf[i], i == 0 ? zero16() : S[PAR ^ 1]);
       else
-        o[h][i % NDB] = mma32(f[q], P[PAR ^ 1][h][i / NDB], o[h][i % NDB]);
-      if (u < SM) {
-        // maximum over elements 16 u / SM .. of both row blocks
+        o[i % NDB] = mma32(f[q], P[PAR ^ 1][i / NDB], o[i % NDB]);
+      if (q < SM) {
+        if (q == 0) mt = sv[0];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-          if (u == 0) mt[j] = sv[j][0];
-#pragma unroll
-          for (int e = 16 * u / SM; e < 16 * (u + 1) / SM; ++e) mt[j] = fmaxf(mt[j], sv[j][e]);
-          if (u == SM - 1) {
-            mt[j] = half_max(mt[j]) * sc;
-            const bool moved = mt[j] > m[j] + 8.f;
-            any |= moved;
-            const float mn = moved ? mt[j] : m[j];
-            mb[j] = mn == -INFINITY ? 0.f : mn;
-            alpha[j] = moved ? __builtin_amdgcn_exp2f(m[j] - mn) : 1.f;   // m = -inf: 0
-            m[j] = mn;
-          }
+        for (int e = 16 * q / SM; e < 16 * (q + 1) / SM; ++e) mt = fmaxf(mt, sv[e]);
+        if (q == SM - 1) {
+          mt = half_max(mt) * sc;
+          moved = mt > m + 8.f;
+          const float mn = moved ? mt : m;
+          mb = mn == -INFINITY ? 0.f : mn;
+          alpha = moved ? __builtin_amdgcn_exp2f(m - mn) : 1.f;   // m = -inf: 0
+          m = mn;
         }
       } else {
 #pragma unroll
-        for (int e = 16 * NJ * (u - SM) / (NS - SM); e < 16 * NJ * (u + 1 - SM) / (NS - SM); ++e) {
-          const int j = e / 16, c = e % 16;
-          p[j][c] = __builtin_amdgcn_exp2f(fmaf(sv[j][c], sc, -mb[j]));   // masked: 0
-          ps[j] += p[j][c];
+        for (int e = 16 * (q - SM) / (NF - SM); e < 16 * (q + 1 - SM) / (NF - SM); ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(sv[e], sc, -mb));   // masked: 0
+          ps += p[e];
           // P is rounded to bf16 for its product; the sum keeps 32 bits
-          if (c % 8 == 7) {
-            pack_frag(P[PAR][j][c / 8], &p[j][c - 7]);
-            asm volatile("" : "+v"(P[PAR][j][c / 8]));   // here, not where the next step reads it
+          if (e % 8 == 7) {
+            pack_frag(P[PAR][e / 8], &p[e - 7]);
+            asm volatile("" : "+v"(P[PAR][e / 8]));   // here, not where the next step reads it
           }
         }
       }
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(ps[j]));
+      asm volatile("" : "+v"(ps));
       __builtin_amdgcn_sched_barrier(0);
     }
+    l = fmaf(l, alpha, ps);
+    if (__ballot(moved)) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) l[j] = fmaf(l[j], alpha[j], ps[j]);
-    if (__ballot(any)) {
+      for (int d = 0; d < NDB; ++d)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
-#pragma unroll
-        for (int d = 0; d < NDB; ++d) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[j][d][i] *= alpha[j];
-          if constexpr (ACC) asm volatile("" : "+a"(o[j][d]));   // 16 at a time, or the compiler asks for 128 registers at once
-        }
+        for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
     }
   };
   // tile t + 1 of V and t + 2 of K (requested a trip ago) go into their stages, and the next ones start to travel
+  int s0 = 0, s1 = 1, s2 = 2;   // the stages of the tiles t, t + 1, t + 2 (and t - 1)
   auto move = [&](int t) {
-    if (t > t0) __syncthreads();
-    if (t + 1 < t1) {
-      hold(tv);
-      tv.store(Vs + stage(t + 1) * TV, LDV, valid_of(t + 1), dh, tid);
-    }
-    if (t + 2 < t1) {
-      hold(tk);
-      tk.store(Ks + stage(t + 2) * TK, LDK, valid_of(t + 2), dh, tid);
+    if (t > 0) __syncthreads();
+    if (t + 1 < nt) tv.store(Vs + s1 * TV, LDV, valid_of(t + 1), dh, tid);
+    if (t + 2 < nt) {
+      tk.store(Ks + s2 * TK, LDK, valid_of(t + 2), dh, tid);
       load_v(t + 2);
     }
-    if (t + 3 < t1) load_k(t + 3);
+    if (t + 3 < nt) load_k(t + 3);
   };
-  for (int t = t0; t < tend; ++t) {
+  auto turn = [&] {
+    const int x = s0;
+    s0 = s1;
+    s1 = s2;
+    s2 = x;
+  };
+  for (int t = 0; t < tend; ++t) {
     move(t);
-    const raw *const Kt = Ks + stage(t) * TK, *const Vt = Vs + stage(t) * TV;
-    step(2 * t, std::integral_constant<int, 0>{}, Kt + 32 * LDK, Vs + (t - t0 + 2) % 3 * TV + 32 * LDV);
-    step(2 * t + 1, std::integral_constant<int, 1>{}, Ks + stage(t + 1) * TK, Vt);
+    const raw *const Kt = Ks + s0 * TK, *const Vt = Vs + s0 * TV;
+    step(2 * t, std::integral_constant<int, 0>{}, Kt + 32 * LDK, Vs + s2 * TV + 32 * LDV);
+    step(2 * t + 1, std::integral_constant<int, 1>{}, Ks + s1 * TK, Vt);
+    turn();
   }
-  if (tend > t0) {   // the last step's products with V
-    const raw* Vp = Vs + stage(tend - 1) * TV + 32 * LDV;
+  if (tend > 0) {   // the last step's products with V
+    const raw* Vp = Vs + s2 * TV + 32 * LDV;
 #pragma unroll
     for (int st = 0; st < 2; ++st)
 #pragma unroll
-      for (int d = 0; d < NDB; ++d) {
-        const bf16x8 vf = col_frag(Vp, LDV, 16 * st + 4 * g, 16 * st + 4 * g + 8, d * 32, lane);
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) o[j][d] = mma32(vf, P[1][j][st], o[j][d]);
-      }
+      for (int d = 0; d < NDB; ++d) o[d] = mma32(col_frag(Vp, LDV, 16 * st + 4 * g, 16 * st + 4 * g + 8, d * 32, lane), P[1][st], o[d]);
   }
-  for (int t = max(tend, t0); t < t1; ++t) move(t);   // (tiles that only the other waves' rows see)
-#pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    float lt = l[j];
-    lt += __shfl_xor(lt, 32, 64);
-    if (wr + j * 32 + r >= rows) continue;
-    const float inv = lt > 0.f ? 1.f / lt : (lt == 0.f ? 0.f : lt);
-    const float lse = lt == 0.f ? -INFINITY : (m[j] + log2f(lt)) * 0.69314718055994530942f;
-    if (a.nsplit) {
-      const long at = (long)(a.part0 + split) * a.total_q * a.H + (long)(s.qbeg + tok[j]) * a.H + head[j];
-      if (g == 0) a.pl[at] = lse;
-      store_row<float, 16, NDB>(a.po + at * a.dhp, o[j], inv, g, dh);
-    } else {
-      if (g == 0 && a.lse) a.lse[(long)head[j] * a.total_q + s.qbeg + tok[j]] = lse;
-      store_row<bf16_t, AL, NDB>((raw*)a.O + (long)(s.qbeg + tok[j]) * a.o_row + (long)head[j] * a.o_head, o[j], inv, g, dh);
-    }
+  for (int t = tend; t < nt; ++t) {   // (tiles that only the other waves' rows see)
+    move(t);
+    turn();
   }
+  l += __shfl_xor(l, 32, 64);
+  if (row >= rows) return;
+  const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);   // nothing seen: zeros; NaN stays
+  const float lse = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+  if (g == 0 && a.lse) a.lse[(long)head * a.total_q + s.qbeg + tok] = lse;
+  store_row<bf16_t, AL, NDB>((raw*)a.O + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head, o, inv, g, dh);
 }
 
 template <typename T, int DH, int AL>
 static void launch_fwd_al(const PackedAttn& a, dim3 grid, hipStream_t s) {
-  if constexpr (DH >= 64 && DH <= 128 && sizeof(T) == 2) {
-    if (a.groups == 4) {
-      packed_fwd_long_kernel<DH, AL, 1, 8><<<grid, 512, 0, s>>>(a);
+  if constexpr (DH == 128 && sizeof(T) == 2) {
+    if (a.tall) {
+      packed_fwd_long_kernel<AL><<<grid, 512, 0, s>>>(a);
       return;
     }
   }
@@ -331,8 +261,8 @@ static void launch_fwd_t(const PackedAttn& a, int align, dim3 grid, hipStream_t 
 }
 void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s) {
   const long rows = (long)a.total_q * a.G;
-  const int bm = a.groups == 4 ? PACKED_BM2 : PACKED_BM;
-  const long slots = a.flat ? (rows + bm - 1) / bm : a.levels ? (long)a.levels * a.nseq : packed_slots(rows, bm, a.nseq);
+  const int bm = a.tall ? PACKED_BM2 : PACKED_BM;
+  const long slots = a.levels ? (long)a.levels * a.nseq : packed_slots(rows, bm, a.nseq);
   const dim3 grid((unsigned)(slots * a.Hk * (a.nsplit > 0 ? a.nsplit : 1)));
   if (bf16)
     launch_fwd_t<bf16_t>(a, align, grid, s);
@@ -341,17 +271,18 @@ void launch_packed_fwd(const PackedAttn& a, int bf16, int align, hipStream_t s) 
 }
 
 // ---------------------------------------------------------------------------------------------------------------------------
-// Joining of the parts: lse = log sum exp lse_p, O = sum_p exp(lse_p - lse) o_p, in part order within each of the lane groups that read parts
-// side by side.  A wave per (token, head); LR lanes hold a row in pieces of four, 64 / LR parts are read at a time.  Reads each part once: bytes,
-// and in small calls the latency of offsets -> lse -> rows, so the parts' lse are read once, a lane each, and handed out by shuffles.
+// Joining of the parts: lse = log sum exp lse_p, O = sum_p exp(lse_p - lse) o_p, in one fixed order.  LR lanes hold a row in pieces of four, so a wave
+// reads 64 / LR parts at a time; WV waves share a (token, head) and meet in LDS.  Reads each part once: bytes, and in small calls the latency of
+// offsets -> lse -> rows, so the parts' lse are read once, a lane each, and handed out by shuffles.
 // ---------------------------------------------------------------------------------------------------------------------------
-template <typename T, int LR>
+template <typename T, int LR, int WV>
 __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
   typedef typename Elem<T>::raw raw;
   constexpr int NP = 64 / LR;
-  const int lane = threadIdx.x & 63;
-  const long id = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (long)a.total_q * a.H) return;   // wave-uniform
+  __shared__ float sm_o[WV > 1 ? 4 : 1][LR * 4], sm_s[WV > 1 ? 4 : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long id = WV > 1 ? (long)blockIdx.x : (long)blockIdx.x * 4 + wave;
+  if (id >= (long)a.total_q * a.H) return;   // uniform among the waves of a row, as all returns below
   const int tokg = (int)(id / a.H), head = (int)(id - (long)tokg * a.H), hk = head / a.G;
   // the token's sequence: the last one that begins at or before it (empty sequences share a begin with the next)
   int lo = 0, n = a.nseq;
@@ -385,16 +316,17 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) mn = fmaxf(mn, __shfl_xor(mn, d, 64));
     mn = fmaxf(mn, mx);
-    if (mn == -INFINITY) continue;
-    const float w = __builtin_amdgcn_exp2f((lp - mn) * 1.44269504088896340736f), alpha = __builtin_amdgcn_exp2f((mx - mn) * 1.44269504088896340736f);
+    const float mb = mn == -INFINITY ? 0.f : mn;   // (nothing seen yet, or NaN alone, which has to stay)
+    const float w = __builtin_amdgcn_exp2f((lp - mb) * 1.44269504088896340736f), alpha = __builtin_amdgcn_exp2f((mx - mb) * 1.44269504088896340736f);
     mx = mn;
     acc *= alpha;
     tot *= alpha;
     const int many = min(64, nall - b);
 #pragma unroll 4
-    for (int q = 0; q < many; q += NP) {
+    for (int q = WV > 1 ? wave * NP : 0; q < many; q += NP * WV) {
       const int p = b + min(q + sub, many - 1);
-      const float wp = q + sub < many ? __shfl(w, q + sub, 64) : 0.f;
+      const float wq = __shfl(w, min(q + sub, 63), 64);   // (of all lanes: a lane that takes no part hands nothing out)
+      const float wp = q + sub < many ? wq : 0.f;
       const float* o = p < a.nparts ? a.po + (p * rows + id) * a.dhp : a.fo + (((long)(few0 + p - a.nparts) * a.Hk + hk) * a.frows + row) * a.dhp;
       const f32x4 v = *(const f32x4*)(o + cc);
       tot += wp;
@@ -408,6 +340,17 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] += __shfl_xor(acc[j], d, 64);
   }
+  if constexpr (WV > 1) {   // (all waves of the row hold the same mx)
+    if (sub == 0) *(f32x4*)&sm_o[wave][c] = acc;
+    if (lane == 0) sm_s[wave] = tot;
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int x = 1; x < WV; ++x) {
+      tot += sm_s[x];
+      acc += *(const f32x4*)&sm_o[x][c];
+    }
+  }
   const float inv = tot == 0.f ? 0.f : 1.f / tot;
   if (lane == 0 && a.lse) a.lse[(long)head * a.total_q + tokg] = tot == 0.f ? -INFINITY : mx + log2f(tot) * 0.69314718055994530942f;
   if (sub == 0) {
@@ -418,23 +361,30 @@ __global__ __launch_bounds__(256) void packed_join_kernel(PackedAttn a) {
   }
 }
 
+template <typename T, int LR>
+static void launch_join(const PackedAttn& a, hipStream_t s) {
+  // Four waves a row where there are few rows, and latency counts: 64 / 1920 rows in 12 / 3 parts 20.0 -> 17.9 / 24.4 -> 20.6 us (with what makes the
+  // parts); 4096 / 7680 rows 23.4 -> 26.1 / 33.8 -> 38.0
+  const long rows = (long)a.total_q * a.H;
+  if (rows < 2048)
+    packed_join_kernel<T, LR, 4><<<dim3((unsigned)rows), 256, 0, s>>>(a);
+  else
+    packed_join_kernel<T, LR, 1><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(a);
+}
+template <typename T>
+static void launch_join_t(const PackedAttn& a, hipStream_t s) {
+  if (a.dh <= 64)
+    launch_join<T, 16>(a, s);
+  else if (a.dh <= 128)
+    launch_join<T, 32>(a, s);
+  else
+    launch_join<T, 64>(a, s);
+}
 void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s) {
-  const dim3 grid((unsigned)(((long)a.total_q * a.H + 3) / 4));
-  if (bf16) {
-    if (a.dh <= 64)
-      packed_join_kernel<bf16_t, 16><<<grid, 256, 0, s>>>(a);
-    else if (a.dh <= 128)
-      packed_join_kernel<bf16_t, 32><<<grid, 256, 0, s>>>(a);
-    else
-      packed_join_kernel<bf16_t, 64><<<grid, 256, 0, s>>>(a);
-  } else {
-    if (a.dh <= 64)
-      packed_join_kernel<float, 16><<<grid, 256, 0, s>>>(a);
-    else if (a.dh <= 128)
-      packed_join_kernel<float, 32><<<grid, 256, 0, s>>>(a);
-    else
-      packed_join_kernel<float, 64><<<grid, 256, 0, s>>>(a);
-  }
+  if (bf16)
+    launch_join_t<bf16_t>(a, s);
+  else
+    launch_join_t<float>(a, s);
 }
 
 }  // namespace sh

@@ -87,6 +87,17 @@ def test_nothing_to_do_is_no_error():
     assert backward(attention(nseq=0)) == b.SH_OK and backward(attention(total_q=0, total_k=0), Q=None, K=None, V=None, O=None, dO=None, lse=None, dQ=None, dK=None, dV=None) == b.SH_OK
 
 
+@pytest.mark.parametrize("over", [dict(nseq=1 << 23, nheads=4096, nkv_heads=4096), dict(nseq=1 << 23, nheads=4096, nkv_heads=4096, max_q=1),
+                                  dict(nheads=64, nkv_heads=64, total_q=1 << 20, max_q=1 << 20)], ids=str)
+def test_grids_that_no_launch_holds(over):
+    """Sizes whose work-groups pass 2^32 threads are refused, not cut."""
+    a = attention(**over)
+    if a.nseq > 3:
+        assert b.switchhead_attention_workspace_bytes(a) == 0 and forward(a) == b.SH_ERR_UNSUPPORTED and backward(a) == b.SH_ERR_UNSUPPORTED
+    else:   # the largest rows that are not joined from parts fit
+        assert b.switchhead_attention_workspace_bytes(a) > 0
+
+
 def test_null_descriptions():
     assert lib().switchhead_attention_workspace_bytes(None, 0) == 0
     assert lib().switchhead_qk_norm_workspace_bytes(None) == 0

@@ -264,6 +264,14 @@ def test_shared_prefix_head_widths(H, Hk, d, dtype):
     Packed(H, Hk, d, dtype, [17, 1, 140], [17, 40, 140], prefix=130, seed=13).check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk,d", [(4, 2, 64), (2, 2, 128), (2, 2, 76), (1, 1, 41), (2, 1, 256)])
+def test_shared_prefix_in_common_tiles(H, Hk, d, dtype):
+    """A prefix much longer than the rows: rows of several sequences share tiles over it, and the own keys are parts of their own."""
+    Packed(H, Hk, d, dtype, [20, 1, 7, 30], [20, 1, 9, 300], prefix=2000, seed=24).check()
+    Packed(H, Hk, d, dtype, [20, 0, 33, 2], [5, 4, 0, 2], prefix=2000, seed=25, gap=2).check()
+
+
 def test_prefix_equals_one_sequence_that_holds_it():
     """A shared prefix in front of one sequence is that sequence with a longer cache."""
     p = Packed(4, 2, 64, "f32", [30], [40], prefix=100, seed=14)
@@ -296,6 +304,66 @@ def test_infinite_and_large_logits():
     got = p.run()
     p.k[5, 0, 0] = -1e30
     close("O", got["O"], p.reference()["O"], "f32")
+
+
+@pytest.mark.parametrize("case", ["chunks", "tiles", "prefix", "prefix tiles"])
+def test_nan_in_a_query_stays(case):
+    """A query of NaN gives NaN, however its keys are split, and touches no other row."""
+    p = {"chunks": lambda: Packed(4, 2, 64, "bf16", [1, 1, 1], [3000, 2, 500], seed=26), "tiles": lambda: Packed(2, 2, 64, "bf16", [40], [3001], seed=27),
+         "prefix": lambda: Packed(4, 2, 64, "bf16", [1, 1, 1], [30, 2, 50], prefix=900, seed=28),
+         "prefix tiles": lambda: Packed(4, 2, 64, "bf16", [20, 10], prefix=3000, seed=29)}[case]()
+    a = p.run()
+    row = p.q.shape[0] - 1
+    p.q[row, 1, 3] = float("nan")
+    b = p.run()
+    assert torch.isnan(b["O"][row, 1]).all() and torch.isnan(b["lse"][1, row])
+    for t in (a, b):
+        t["O"][row, 1], t["lse"][1, row] = 0, 0
+    assert torch.equal(a["O"], b["O"]) and torch.equal(a["lse"], b["lse"])
+
+
+@pytest.mark.parametrize("H,Hk,d,queries,keys,prefix,causal,fused", [
+    (48, 12, 128, [4096, 1, 300], None, 0, 1, False), (64, 64, 128, [4100, 77], [4100, 4500], 0, 1, False), (48, 48, 100, [4097], None, 0, 1, True),
+    (33, 33, 101, [6000, 500], [6100, 100], 0, 1, False), (64, 16, 128, [5000], [3900], 300, 1, False), (16, 16, 128, [12300], [4200], 0, 0, False)])
+def test_long_rows_in_tall_tiles(H, Hk, d, queries, keys, prefix, causal, fused):
+    """Enough long rows for tiles of 256: every head of some, against float64 (one head at a time on the GPU)."""
+    keys = queries if keys is None else keys
+    p = Packed(H, Hk, d, "bf16", queries, keys, causal, prefix, seed=30, fused=fused)
+    got = p.run()
+    w = lambda t: t.cuda().double()
+    for i, (n, m) in enumerate(zip(queries, keys)):
+        qs, ks = slice(p.qoff[i], p.qoff[i] + n), slice(p.koff[i], p.koff[i] + m)
+        hidden = torch.arange(m, device="cuda")[None] > (m - n) + torch.arange(n, device="cuda")[:, None] if causal else torch.zeros(n, m, dtype=torch.bool, device="cuda")
+        if prefix:
+            hidden = torch.cat((torch.zeros(n, prefix, dtype=torch.bool, device="cuda"), hidden), 1)
+        for h in sorted({0, H // 2, H - 1}):
+            hk = h // (H // Hk)
+            k, v = w(p.k[ks, hk]), w(p.v[ks, hk])
+            if prefix:
+                k, v = torch.cat((w(p.kp[:, hk]), k)), torch.cat((w(p.vp[:, hk]), v))
+            s = (w(p.q[qs, h]) @ k.t().contiguous() * p.scale).masked_fill_(hidden, NEG)
+            close("lse", got["lse"][h, qs], torch.logsumexp(s, 1).cpu(), "f32")
+            close("O", got["O"][qs, h], (torch.nan_to_num(torch.softmax(s, 1)) @ v).cpu(), "bf16")
+
+
+def test_calls_on_two_streams():
+    """Two calls at once, each with its stream and workspace."""
+    ps = [Packed(8, 2, 128, "bf16", [130, 257, 1, 64], seed=31), Packed(4, 4, 64, "bf16", [1] * 5, [3000, 5, 70, 900, 1], seed=32)]
+    alone = [p.run() for p in ps]
+    streams, runs = [torch.cuda.Stream() for _ in ps], []
+    for p, s in zip(ps, streams):
+        q, k, v = p.device()
+        O, off = torch.zeros_like(q), [torch.tensor(x, dtype=torch.int32, device="cuda") for x in (p.qoff, p.koff)]
+        plan = binding.make_attention(q, k, v, O, len(p.nq), max(p.nq), max(p.nk))
+        runs.append((s, plan, q, k, v, *off, O, torch.empty(binding.switchhead_attention_workspace_bytes(plan), dtype=torch.uint8, device="cuda")))
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, plan, q, k, v, qo, ko, O, ws in runs:
+            with torch.cuda.stream(s):
+                binding.switchhead_attention_forward(plan, q, k, v, qo, ko, O, None, ws)
+    torch.cuda.synchronize()
+    for a, r in zip(alone, runs):
+        assert torch.equal(a["O"], r[7])
 
 
 def test_bounds_on_the_lengths():
