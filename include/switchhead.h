@@ -349,7 +349,7 @@ sh_status switchhead_qk_norm_rope_backward(const sh_qk_norm* a, const void* Q, c
  * 0 < T_q < T the first T - T_q rows of x are a prefix that every sequence sees in front of its own rows: keys and values
  * of it are computed once, queries and y exist for the T_q rows behind it.  With shape->rope positions count within the
  * sequence, from 0 or behind the prefix.  Rows that belong to no sequence take no part: their y and dx are 0, and the weights' gradients
- * have nothing of them (their routing is computed like every row's).
+ * have nothing of them (their routing is computed like every row's, so what x and dy hold there must be finite).
  */
 typedef struct {
   int32_t nseq;                 /* >= 1                                                                              */

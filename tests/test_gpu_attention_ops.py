@@ -346,6 +346,28 @@ def test_long_rows_in_tall_tiles(H, Hk, d, queries, keys, prefix, causal, fused)
             close("O", got["O"][qs, h], (torch.nan_to_num(torch.softmax(s, 1)) @ v).cpu(), "bf16")
 
 
+@pytest.mark.parametrize("H,Hk,d", [(2, 2, 64), (4, 1, 128), (1, 1, 256)])
+def test_more_parts_than_lanes(H, Hk, d):
+    """A token over so many chunks of keys that the joining wave takes their sums in several rounds."""
+    Packed(H, Hk, d, "bf16", [1], [20000], seed=33).check()
+    Packed(H, Hk, d, "f32", [1, 2], [17001, 300], seed=34).check()
+
+
+def test_backward_in_ranges_of_rows():
+    """Few key tiles and many rows: dK and dV from several ranges of rows."""
+    Packed(8, 2, 128, "bf16", [700, 5], seed=35).check(backward=True)
+    Packed(6, 1, 76, "bf16", [500], [300], seed=36, causal=0).check(backward=True)
+
+
+def test_backward_that_keeps_no_score_gradients():
+    """More keys and rows than score gradients are kept for: dQ computes them again."""
+    p = Packed(4, 1, 32, "bf16", [300, 1], seed=37)
+    p.k, p.v = (torch.cat((t, torch.full((1 << 20, 1, 32), 3.0, dtype=t.dtype))) for t in (p.k, p.v))   # rows of no sequence
+    plan = binding.make_attention(p.q, p.k, p.v, p.q, 2, 300, 300)
+    assert binding.switchhead_attention_workspace_bytes(plan, True) < p.k.shape[0] * 1200 * 2
+    p.check(backward=True)
+
+
 def test_calls_on_two_streams():
     """Two calls at once, each with its stream and workspace."""
     ps = [Packed(8, 2, 128, "bf16", [130, 257, 1, 64], seed=31), Packed(4, 4, 64, "bf16", [1] * 5, [3000, 5, 70, 900, 1], seed=32)]
