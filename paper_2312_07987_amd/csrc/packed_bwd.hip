@@ -185,7 +185,7 @@ __device__ __forceinline__ bool key_tile(const PackedAttnBwd& b, int id, int& nt
 // kind per SIMD; three stages for the row tiles (written a trip ahead, read by the score waves in the next trip and by the gradient waves
 // in the one after), two hand-over buffers, one barrier per 64 rows.  A score wave has four chains of products in flight (two blocks of 32
 // rows, S and dP): with one block per trip the chain barrier, fragment reads, products, exponentials, barrier was what a trip waited for.
-// A gradient wave owns 64 keys and half of d where d has an even number of 32-wide blocks, so that a fragment serves two products.
+// A gradient wave owns dK or dV of 64 keys, so that a fragment of the rows serves two products: the LDS pipe is what bounds a trip.
 // (Q and dO straight from memory in operand order for the score waves: 32 rows of 32 bytes an instruction are more than the vector memory path
 // carries, dK / dV of 16384 tokens 180 -> 329 us.)
 // Heads of 97 .. 128: rows of 256 bytes whose 16-byte pieces are permuted by the row (swizzle), so that both the 16 rows of a fragment read and the
@@ -196,8 +196,6 @@ template <int DH, int AL>
 __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) {
   const PackedAttn& a = b.f;
   constexpr int QT = PACKED_QT, KB = PACKED_KB, LD = DH == 128 ? 128 : DH + 16, NST = 3, NKD = DH / 16, NDB = DH / 32, CPR = DH / 8, TOTAL = QT * CPR, NCH = (TOTAL + 255) / 256;
-  constexpr bool HALF = NDB % 2 == 0;                      // a gradient wave: 64 keys x half of d, or 32 keys x all of d
-  constexpr int KBW = HALF ? 2 : 1, DW = HALF ? NDB / 2 : NDB;
   constexpr int STAGE = 2 * QT * LD;
   __shared__ __attribute__((aligned(16))) unsigned short tiles[NST * STAGE];
   __shared__ __attribute__((aligned(16))) uint4 hand[2][4][8][64];   // [buffer][key block][P, dS of 16 rows in turn][lane]
@@ -235,7 +233,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
     mem_frags<bf16_t, AL, NKD, 16>(kf, (const raw16*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head, 8 * g, dh, key < s.lk);
     mem_frags<bf16_t, AL, NKD, 16>(vf, (const raw16*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head, 8 * g, dh, key < s.lk);
     // (keys past the sequence have no row of dS^T: they repeat the last key's address and do not store)
-    raw16* const dsrow = (raw16*)b.dS + (b.dS ? ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 4 * g : 0);
+    raw16* const dsrow = (raw16*)b.dS + (b.dS ? ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 8 * g : 0);
     const bool ds_store = b.dS && key < s.lk;
     const float sc = a.scale * 1.44269504088896340736f;
     // the statistics of the next tile's rows (lane half 0: lse, 1: delta; rows past the end repeat the last one)
@@ -314,16 +312,14 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
           union {
             bf16x8 v;
             uint4 q;
-            uint2 hh[2];
           } up, ud;
           pack_frag(up.v, &p[8 * h]);
           pack_frag(ud.v, &ds[8 * h]);
           hd[2 * h * 64] = up.q;
           hd[(2 * h + 1) * 64] = ud.q;
-          if (ds_store) {   // elements 0..3 / 4..7: rows r0 + 16 h + 4 g + {0..3} / + 8 + {0..3} of this lane's key
-            *(uint2*)(dsrow + r0 + 16 * h) = ud.hh[0];
-            *(uint2*)(dsrow + r0 + 16 * h + 8) = ud.hh[1];
-          }
+          // elements 0..3 / 4..7: rows r0 + 16 h + 4 g + {0..3} / + 8 + {0..3} of this lane's key; the lane halves trade, so that each has 8 rows side by side
+          const auto lo = __builtin_amdgcn_permlane32_swap(ud.q.x, ud.q.z, false, false), hi = __builtin_amdgcn_permlane32_swap(ud.q.y, ud.q.w, false, false);
+          if (ds_store) *(uint4*)(dsrow + r0 + 16 * h) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
         }
       }
     }
@@ -331,7 +327,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
   }
 
   const int gt = tid - 256, gw = wave - 4;
-  const int kb0 = HALF ? (gw & 1) * 2 : gw, d0 = HALF ? (gw >> 1) * DW : 0;   // the wave's key blocks and d blocks
+  const int kb0 = (gw >> 1) * 2, of_k = gw & 1;   // the wave's two key blocks; dK or dV
   uint4 tq[NCH], tg[NCH];
   auto prefetch = [&](int r0) {   // (rows past the end repeat the last one)
 #pragma unroll
@@ -370,11 +366,11 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
     u.half[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(LDS_PTR(s16x4, tile + (row + 8) * LD + piece(row + 8, p) * 8 + in));
     return u.v;
   };
-  f32x16 accK[KBW][DW], accV[KBW][DW];
+  f32x16 acc[2][NDB];
 #pragma unroll
-  for (int k = 0; k < KBW; ++k)
+  for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int d = 0; d < DW; ++d) accK[k][d] = accV[k][d] = zero16();
+    for (int d = 0; d < NDB; ++d) acc[k][d] = zero16();
   if (n > 0) {
     prefetch(rbeg);
     stage(tiles, rbeg);
@@ -388,8 +384,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
       if (it + 2 < n) prefetch(rbeg + (it + 2) * QT);
     }
     if (it == 0) continue;
-    const raw16* Qt = tiles + (it - 1) % NST * STAGE;
-    const raw16* Gt = Qt + QT * LD;
+    const raw16* tile = tiles + (it - 1) % NST * STAGE + (of_k ? 0 : QT * LD);   // dK: Q, dV: dO
     const int left = rend - (rbeg + (it - 1) * QT);   // rows of the tile that exist
 #pragma unroll
     for (int h = 0; h < QT / 16; ++h) {
@@ -397,42 +392,33 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
       union {
         uint4 q;
         bf16x8 v;
-      } up[KBW], ud[KBW];
+      } w[2];   // dK: dS, dV: P
 #pragma unroll
-      for (int k = 0; k < KBW; ++k) {
-        up[k].q = hand[(it - 1) & 1][kb0 + k][2 * h][lane];
-        ud[k].q = hand[(it - 1) & 1][kb0 + k][2 * h + 1][lane];
-      }
+      for (int k = 0; k < 2; ++k) w[k].q = hand[(it - 1) & 1][kb0 + k][2 * h + of_k][lane];
 #pragma unroll
-      for (int d = 0; d < DW; ++d) {
-        const bf16x8 gfr = columns(Gt, h, d0 + d), qfr = columns(Qt, h, d0 + d);
+      for (int d = 0; d < NDB; ++d) {
+        const bf16x8 f = columns(tile, h, d);
 #pragma unroll
-        for (int k = 0; k < KBW; ++k) {
-          accV[k][d] = mma32(gfr, up[k].v, accV[k][d]);
-          accK[k][d] = mma32(qfr, ud[k].v, accK[k][d]);
-        }
+        for (int k = 0; k < 2; ++k) acc[k][d] = mma32(f, w[k].v, acc[k][d]);
       }
     }
   }
 #pragma unroll
-  for (int k = 0; k < KBW; ++k) {
+  for (int k = 0; k < 2; ++k) {
     const int key = k0 + (kb0 + k) * 32 + r;
     if (p0 == p1) {
       if (key < s.lk) {
-        store_row<bf16_t, AL, DW>((raw16*)b.dK + (long)(s.kbeg + key) * a.k_row + (long)hk * a.k_head + d0 * 32, accK[k], a.scale, g, dh - d0 * 32);
-        store_row<bf16_t, AL, DW>((raw16*)b.dV + (long)(s.kbeg + key) * a.v_row + (long)hk * a.v_head + d0 * 32, accV[k], 1.f, g, dh - d0 * 32);
+        raw16* const out = of_k ? (raw16*)b.dK + (long)(s.kbeg + key) * a.k_row + (long)hk * a.k_head : (raw16*)b.dV + (long)(s.kbeg + key) * a.v_row + (long)hk * a.v_head;
+        store_row<bf16_t, AL, NDB>(out, acc[k], of_k ? a.scale : 1.f, g, dh);
       }
       continue;
     }
-    // a part: accumulators in register order, 16 bytes per lane, by key block and d block
-    f32x4* out = (f32x4*)(b.dkv + ((long)part * b.kslots + (long)slot * a.Hk + hk) * b.dkv_floats) + ((kb0 + k) * NDB + d0) * 4 * 64 + lane;
+    // a part: accumulators in register order, 16 bytes per lane, by key block and d block, dV first
+    f32x4* out = (f32x4*)(b.dkv + ((long)part * b.kslots + (long)slot * a.Hk + hk) * b.dkv_floats) + (of_k * 4 + kb0 + k) * NDB * 4 * 64 + lane;
 #pragma unroll
-    for (int d = 0; d < DW; ++d)
+    for (int d = 0; d < NDB; ++d)
 #pragma unroll
-      for (int i4 = 0; i4 < 4; ++i4) {
-        out[(d * 4 + i4) * 64] = f32x4{accV[k][d][4 * i4], accV[k][d][4 * i4 + 1], accV[k][d][4 * i4 + 2], accV[k][d][4 * i4 + 3]};
-        out[(4 * NDB * 4 + d * 4 + i4) * 64] = f32x4{accK[k][d][4 * i4], accK[k][d][4 * i4 + 1], accK[k][d][4 * i4 + 2], accK[k][d][4 * i4 + 3]};
-      }
+      for (int i4 = 0; i4 < 4; ++i4) out[(d * 4 + i4) * 64] = f32x4{acc[k][d][4 * i4], acc[k][d][4 * i4 + 1], acc[k][d][4 * i4 + 2], acc[k][d][4 * i4 + 3]};
   }
 }
 
