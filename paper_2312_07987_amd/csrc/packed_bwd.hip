@@ -179,23 +179,28 @@ __device__ __forceinline__ bool key_tile(const PackedAttnBwd& b, int id, int& nt
 }
 
 // The same for bf16 heads of up to 128 elements with two kinds of waves.  A single wave per SIMD, which is all that the kernel above has registers
-// for, leaves the matrix cores idle during exponentials, conversions and LDS traffic.  Here waves 0 .. 3 (score) hold the K and V fragments
-// of 32 keys each, form P and dS of a tile of 64 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
+// for, leaves the matrix cores idle during exponentials, conversions and LDS traffic.  Here waves 0 .. 3 (score) hold K and V fragments,
+// form P and dS of a tile of 64 rows and leave both as bf16 operand fragments in LDS (and dS^T in memory for dQ); waves
 // 4 .. 7 (gradient) hold the dK and dV accumulators, add the previous tile's products, and move the row tiles from memory to LDS.  One of each
 // kind per SIMD; three stages for the row tiles (written a trip ahead, read by the score waves in the next trip and by the gradient waves
-// in the one after), two hand-over buffers, one barrier per 64 rows.  A score wave has four chains of products in flight (two blocks of 32
-// rows, S and dP): with one block per trip the chain barrier, fragment reads, products, exponentials, barrier was what a trip waited for.
-// A gradient wave owns dK or dV of 64 keys, so that a fragment of the rows serves two products: the LDS pipe is what bounds a trip.
+// in the one after), two hand-over buffers, one barrier per 64 rows.  A score wave has four chains of products in flight (S and dP of two blocks of 32 x 32):
+// with one block per trip the chain barrier, fragment reads, products, exponentials, barrier was what a trip waited for.  Up to 96 elements the two
+// blocks are of two key blocks, so that a fragment of the rows serves both (6600 tokens, 20 heads of 80 over 4, 415 -> 390 us); of 128 the K and V fragments
+// of two do not fit the registers (163 -> 190), and they are of two row blocks.
+// A gradient wave owns dK or dV of 64 keys, so that a fragment of the rows serves two products there.
 // (Q and dO straight from memory in operand order for the score waves: 32 rows of 32 bytes an instruction are more than the vector memory path
 // carries, dK / dV of 16384 tokens 180 -> 329 us.)
 // Heads of 97 .. 128: rows of 256 bytes whose 16-byte pieces are permuted by the row (swizzle), so that both the 16 rows of a fragment read and the
 // 4 rows x 64 bytes of a transposing read fall on all banks, and three stages and two buffers fill the 160 KB.  Narrower ones are padded.
 // Under a causal mask the first keys of a sequence are seen by all of its rows, the last by few, so rows are cut into ranges of rchunk
 // and a (key tile, range) is a work-group; ranges that are the only one of their tile write dK and dV, others fp32 parts.
+// Measured: 16 x 2048 tokens, 8 heads of 128, 485 us, 566 TFLOP/s; without the exponentials 453, without storing dS^T 413, without moving the row tiles 431,
+// without all three 316: a trip is the sum of what its two kinds of waves cannot hide from each other, half of it matrix instructions.
 template <int DH, int AL>
 __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) {
   const PackedAttn& a = b.f;
   constexpr int QT = PACKED_QT, KB = PACKED_KB, LD = DH == 128 ? 128 : DH + 16, NST = 3, NKD = DH / 16, NDB = DH / 32, CPR = DH / 8, TOTAL = QT * CPR, NCH = (TOTAL + 255) / 256;
+  constexpr int SK = DH <= 96 ? 2 : 1, SR = QT / 32 / SK;   // key blocks and row blocks of a score wave
   constexpr int STAGE = 2 * QT * LD;
   __shared__ __attribute__((aligned(16))) unsigned short tiles[NST * STAGE];
   __shared__ __attribute__((aligned(16))) uint4 hand[2][4][8][64];   // [buffer][key block][P, dS of 16 rows in turn][lane]
@@ -228,21 +233,25 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
   auto piece = [](int row, int p) { return DH == 128 ? p ^ ((row & 3) << 2 | (row >> 2 & 1) << 1 | (row >> 3 & 1)) : p; };
 
   if (wave < 4) {
-    const int key = k0 + wave * 32 + r, wk_first = k0 + wave * 32;
-    bf16x8 kf[NKD], vf[NKD];
-    mem_frags<bf16_t, AL, NKD, 16>(kf, (const raw16*)a.K + (long)(s.kbeg + min(key, s.lk - 1)) * a.k_row + (long)hk * a.k_head, 8 * g, dh, key < s.lk);
-    mem_frags<bf16_t, AL, NKD, 16>(vf, (const raw16*)a.V + (long)(s.kbeg + min(key, s.lk - 1)) * a.v_row + (long)hk * a.v_head, 8 * g, dh, key < s.lk);
+    const int kb0 = SK == 2 ? (wave & 1) * 2 : wave, b0 = SK == 2 ? wave >> 1 : 0;   // the wave's key blocks, and its blocks of 32 of a tile's rows
+    bf16x8 kf[SK][NKD], vf[SK][NKD];
     // (keys past the sequence have no row of dS^T: they repeat the last key's address and do not store)
-    raw16* const dsrow = (raw16*)b.dS + (b.dS ? ((long)hk * a.total_k + s.kbeg + min(key, s.lk - 1)) * b.ds_ld + 8 * g : 0);
-    const bool ds_store = b.dS && key < s.lk;
+    raw16* dsrow[SK];
+#pragma unroll
+    for (int k = 0; k < SK; ++k) {
+      const int key = k0 + (kb0 + k) * 32 + r, kc = s.kbeg + min(key, s.lk - 1);
+      mem_frags<bf16_t, AL, NKD, 16>(kf[k], (const raw16*)a.K + (long)kc * a.k_row + (long)hk * a.k_head, 8 * g, dh, key < s.lk);
+      mem_frags<bf16_t, AL, NKD, 16>(vf[k], (const raw16*)a.V + (long)kc * a.v_row + (long)hk * a.v_head, 8 * g, dh, key < s.lk);
+      dsrow[k] = (raw16*)b.dS + (b.dS ? ((long)hk * a.total_k + kc) * b.ds_ld + 8 * g : 0);
+    }
     const float sc = a.scale * 1.44269504088896340736f;
     // the statistics of the next tile's rows (lane half 0: lse, 1: delta; rows past the end repeat the last one)
-    float st[QT / 32];
+    float st[SR];
     auto statistics = [&](int r0) {
 #pragma unroll
-      for (int blk = 0; blk < QT / 32; ++blk) {
+      for (int blk = 0; blk < SR; ++blk) {
         int tok, head;
-        place(min(r0 + blk * 32 + r, rows - 1), tok, head);
+        place(min(r0 + (b0 + blk) * 32 + r, rows - 1), tok, head);
         st[blk] = (g ? b.delta : a.lse)[(long)head * a.total_q + tok];
       }
     };
@@ -253,26 +262,31 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
       const raw16* Qr = tiles + it % NST * STAGE;
       const raw16* Gr = Qr + QT * LD;
       // the statistics go through the start of the wave's own hand-over place, which is not written before they are read
-      uint4* const place_ = hand[it & 1][wave][0];
-      float* const sl = (float*)place_;
+      float* const sl = (float*)hand[it & 1][kb0][b0 * 4];
 #pragma unroll
-      for (int blk = 0; blk < QT / 32; ++blk) sl[(blk * 2 + g) * 32 + r] = g ? st[blk] : st[blk] * 1.44269504088896340736f;
+      for (int blk = 0; blk < SR; ++blk) sl[(blk * 2 + g) * 32 + r] = g ? st[blk] : st[blk] * 1.44269504088896340736f;
       if (it + 1 < n) statistics(rbeg + (it + 1) * QT);
-      f32x16 S_[QT / 32], dP_[QT / 32];
+      f32x16 S_[SR][SK], dP_[SR][SK];
 #pragma unroll
-      for (int blk = 0; blk < QT / 32; ++blk) S_[blk] = dP_[blk] = zero16();
+      for (int blk = 0; blk < SR; ++blk)
+#pragma unroll
+        for (int k = 0; k < SK; ++k) S_[blk][k] = dP_[blk][k] = zero16();
 #pragma unroll
       for (int kk = 0; kk < NKD; ++kk)
 #pragma unroll
-        for (int blk = 0; blk < QT / 32; ++blk) {
-          const int at = (blk * 32 + r) * LD + piece(r, 2 * kk + g) * 8;
-          S_[blk] = mma32(row_frag(Qr + at), kf[kk], S_[blk]);
-          dP_[blk] = mma32(row_frag(Gr + at), vf[kk], dP_[blk]);
+        for (int blk = 0; blk < SR; ++blk) {
+          const int at = ((b0 + blk) * 32 + r) * LD + piece(r, 2 * kk + g) * 8;
+          const bf16x8 q = row_frag(Qr + at), x = row_frag(Gr + at);
+#pragma unroll
+          for (int k = 0; k < SK; ++k) {
+            S_[blk][k] = mma32(q, kf[k][kk], S_[blk][k]);
+            dP_[blk][k] = mma32(x, vf[k][kk], dP_[blk][k]);
+          }
         }
       wave_order();
-      f32x4 L_[QT / 32][4], D_[QT / 32][4];
+      f32x4 L_[SR][4], D_[SR][4];
 #pragma unroll
-      for (int blk = 0; blk < QT / 32; ++blk)
+      for (int blk = 0; blk < SR; ++blk)
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
           L_[blk][i4] = *(const f32x4*)&sl[blk * 64 + 8 * i4 + 4 * g];
@@ -280,46 +294,45 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
         }
       wave_order();
 #pragma unroll
-      for (int blk = 0; blk < QT / 32; ++blk) {
-        const int r0 = rbeg + it * QT + blk * 32;
+      for (int blk = 0; blk < SR; ++blk) {
+        const int r0 = rbeg + it * QT + (b0 + blk) * 32;
         if (r0 >= rend) break;   // uniform
-        const f32x16 S = S_[blk], dP = dP_[blk];
-        float p[16], ds[16];
 #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const f32x4 L = L_[blk][i4], D = D_[blk][i4];
-#pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const int i = 4 * i4 + t;
-            p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L[t]));
-            ds[i] = p[i] * (dP[i] - D[t]);
-          }
-        }
-        // wave-uniform: most blocks lie wholly inside the visible region
-        if (r0 + 32 > rend || wk_first + 32 > s.lk || (a.causal && wk_first + 31 > div_by(r0, a.g_inv) + off)) {
+        for (int k = 0; k < SK; ++k) {
+          const int wk = k0 + (kb0 + k) * 32, key = wk + r;
+          const f32x16 S = S_[blk][k], dP = dP_[blk][k];
+          float p[16], ds[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int rr = r0 + 8 * (i >> 2) + 4 * g + (i & 3);
-            const bool vis = rr < rend && key < s.lk && (!a.causal || key <= div_by(rr, a.g_inv) + off);
-            p[i] = vis ? p[i] : 0.f;
-            ds[i] = vis ? ds[i] : 0.f;
+            p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L_[blk][i / 4][i % 4]));
+            ds[i] = p[i] * (dP[i] - D_[blk][i / 4][i % 4]);
           }
-        }
-        // P and dS are rounded to bf16 here, once, for their products
-        uint4* hd = hand[it & 1][wave][blk * 4] + lane;
+          // wave-uniform: most blocks lie wholly inside the visible region
+          if (r0 + 32 > rend || wk + 32 > s.lk || (a.causal && wk + 31 > div_by(r0, a.g_inv) + off)) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          union {
-            bf16x8 v;
-            uint4 q;
-          } up, ud;
-          pack_frag(up.v, &p[8 * h]);
-          pack_frag(ud.v, &ds[8 * h]);
-          hd[2 * h * 64] = up.q;
-          hd[(2 * h + 1) * 64] = ud.q;
-          // elements 0..3 / 4..7: rows r0 + 16 h + 4 g + {0..3} / + 8 + {0..3} of this lane's key; the lane halves trade, so that each has 8 rows side by side
-          const auto lo = __builtin_amdgcn_permlane32_swap(ud.q.x, ud.q.z, false, false), hi = __builtin_amdgcn_permlane32_swap(ud.q.y, ud.q.w, false, false);
-          if (ds_store) *(uint4*)(dsrow + r0 + 16 * h) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+            for (int i = 0; i < 16; ++i) {
+              const int rr = r0 + 8 * (i >> 2) + 4 * g + (i & 3);
+              const bool vis = rr < rend && key < s.lk && (!a.causal || key <= div_by(rr, a.g_inv) + off);
+              p[i] = vis ? p[i] : 0.f;
+              ds[i] = vis ? ds[i] : 0.f;
+            }
+          }
+          // P and dS are rounded to bf16 here, once, for their products
+          uint4* hd = hand[it & 1][kb0 + k][(b0 + blk) * 4] + lane;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            union {
+              bf16x8 v;
+              uint4 q;
+            } up, ud;
+            pack_frag(up.v, &p[8 * h]);
+            pack_frag(ud.v, &ds[8 * h]);
+            hd[2 * h * 64] = up.q;
+            hd[(2 * h + 1) * 64] = ud.q;
+            // elements 0..3 / 4..7: rows r0 + 16 h + 4 g + {0..3} / + 8 + {0..3} of this lane's key; the lane halves trade, so that each has 8 rows side by side
+            const auto lo = __builtin_amdgcn_permlane32_swap(ud.q.x, ud.q.z, false, false), hi = __builtin_amdgcn_permlane32_swap(ud.q.y, ud.q.w, false, false);
+            if (b.dS && key < s.lk) *(uint4*)(dsrow[k] + r0 + 16 * h) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+          }
         }
       }
     }
