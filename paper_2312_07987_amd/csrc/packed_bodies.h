@@ -228,7 +228,8 @@ __device__ __forceinline__ void packed_fwd_body(const PackedAttn& a, int b, type
 //   O^T[d][row] += V^T P^T      a lane's scores of a piece's two blocks of 16 keys (4 g .. 4 g + 3 of each) are its operand as they are; V goes
 //                               through the wave's own LDS and is read by columns in that key order
 // The waves take every fourth piece of 32 keys without barriers; a piece's registers are requested again as soon as they are free and
-// travel during the softmax and the second product.  Bound by reading K and V once.
+// travel during the softmax and the second product.  Bound by reading K and V once: 32 tokens over 2000 .. 32768 keys, 8 kv heads of 128, 220 us,
+// 4.5 TB/s (a large copy 5.06); 16 over 500 .. 4000, 4 kv heads, 14 us, 4.4 TB/s.
 // ---------------------------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ f32x4 mma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mma16(f32x8 a, f32x8 b, f32x4 c) {
@@ -414,6 +415,5 @@ __device__ __forceinline__ void packed_few_body(const PackedAttn& a, int block, 
     }
   }
 }
-
 
 }  // namespace sh

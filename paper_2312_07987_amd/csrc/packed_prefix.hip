@@ -1,6 +1,7 @@
 // Sequences that share a prefix, where each has few rows: the prefix in tiles of the rows of all sequences, read once for all, and the sequences' own keys
 // as parts of their own, both in one launch: the first work-groups take the prefix, the others the sequences (one after the other in two launches the
-// smaller one leaves most of the chip idle: 64 single tokens over 4096 shared keys and up to 500 of their own 17 + 11 us).
+// smaller one leaves most of the chip idle: 64 single tokens over 4096 shared keys and up to 500 of their own 17 + 11 us,
+// together 21).  Bound by the chain of key tiles that a wave walks, and for few rows by the prefix' bytes.
 #include "packed_bodies.h"
 
 namespace sh {
