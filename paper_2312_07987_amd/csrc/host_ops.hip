@@ -210,8 +210,8 @@ BwdPlan plan_backward(const AttnPlan& p) {
   if (a.dtype == SH_BF16 && a.d_head <= 128 && rows > 0) {
     // Rows of a dK / dV work-group: what a CU would get if every key tile were seen by the longest rows there are.  Parts cost their writing and a second
     // kernel, so they are for launches with a few tiles far longer than the rest.  A step with 100 / 50 / 35 / 20 per cent of this, us: 16384 tokens
-    // of 4 heads of 128, longest 4096, 334 (no parts) / 366 / 366 / 394; 6600 tokens of 20 heads over 4, longest 4096, 688 / 719 / 709 / 714 (860 without
-    // parts).  At least 512, where a work-group is about as long as its start and the extra parts.
+    // of 4 heads of 128, longest 4096, 304 (297 without parts) / 334 / 336 / 359; 6600 tokens of 20 heads over 4, longest 4096, 597 / 629 / 623 / 637 (743 without
+    // parts); 4096 tokens of 8 heads over 2 311 / 322 / 327 / 350 (639).  At least 512, where a work-group is about as long as its start and the extra parts.
     const long tiles = ceil_div(a.total_k, PACKED_KB) * a.nkv_heads;
     long chunk = tiles * rows / 256;
     chunk = ceil_div(chunk < 512 ? 512 : chunk, PACKED_QT) * PACKED_QT;
