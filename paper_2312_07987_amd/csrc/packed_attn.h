@@ -85,8 +85,9 @@ __device__ __forceinline__ SeqGeom seq_geom(const PackedAttn& a, int i) {
 __device__ __forceinline__ int first_slot(const int* off, int total, int mul, int tile, int i) {
   return (int)((unsigned)(clamp_to(off[i], 0, total) * mul) / (unsigned)tile) + i;
 }
-// The sequence of a slot, the slot's number within it and the sequence's places; false for slots ahead of the first sequence.  KEYS: slots of
-// `tile` keys, else of `tile` rows of G per query.  In the last round, where the lanes' sequences are neighbours, every lane reads its
+// The sequence of a slot, the slot's number within it and the sequence's places; false for slots that hold nothing: ahead of the first sequence, behind
+// the last tile of theirs, and, where offsets fall and the slots' order means nothing, any that is no tile of the sequence it leads to (its number may
+// be negative or past 2^31 / tile).  KEYS: slots of `tile` keys, else of `tile` rows of G per query.  In the last round, where the lanes' sequences are neighbours, every lane reads its
 // sequence's places along with the offset, so that up to 64 sequences cost one trip to memory.  All 64 lanes must take part.
 template <bool KEYS>
 __device__ __forceinline__ bool find_slot(const PackedAttn& a, int tile, int slot, int& nth, SeqGeom& s) {
@@ -112,7 +113,7 @@ __device__ __forceinline__ bool find_slot(const PackedAttn& a, int tile, int slo
   s.lq = __builtin_amdgcn_readlane(mine.lq, k);
   s.kbeg = __builtin_amdgcn_readlane(mine.kbeg, k);
   s.lk = __builtin_amdgcn_readlane(mine.lk, k);
-  return true;
+  return nth >= 0 && (long)nth * tile < (KEYS ? s.lk : s.lq * mul);
 }
 
 __device__ __forceinline__ int level_seq(int id, int nseq) { return (id % nseq + id / nseq) % nseq; }

@@ -47,9 +47,7 @@ __device__ __forceinline__ void packed_fwd_body(const PackedAttn& a, int b, type
     int nth;
     if (!find_slot<false>(a, BM, slot, nth, s)) return;
     // the last tiles, which see most keys, first
-    const int nt = (s.lq * a.G + BM - 1) / BM;
-    if (nth >= nt) return;
-    row0 = (nt - 1 - nth) * BM;
+    row0 = ((s.lq * a.G + BM - 1) / BM - 1 - nth) * BM;
   }
   const int rows = s.lq * a.G;
   if (row0 >= rows) return;
@@ -280,7 +278,7 @@ __device__ __forceinline__ void packed_few_body(const PackedAttn& a, int block, 
   }
   const int rows = s.lq * a.G;   // at most frows = max_q * G <= 16
   const int key0 = nth * a.chunk, kend = a.chunk ? min(s.lk, key0 + a.chunk) : s.lk;
-  if (rows <= 0 || (a.chunk && key0 >= s.lk)) return;   // (unsplit, a sequence without keys still gets its zeros)
+  if (rows <= 0) return;   // (unsplit, a sequence without keys still gets its zeros)
   const int off = s.lk - s.lq;
   const int rc = min(r, rows - 1), tok = div_by(rc, a.g_inv), head = hk * a.G + rc - tok * a.G;
   const raw* const K = (const raw*)a.K + (long)s.kbeg * a.k_row + (long)hk * a.k_head;

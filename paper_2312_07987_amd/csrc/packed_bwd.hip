@@ -17,7 +17,7 @@ __device__ __forceinline__ bool row_tile(const PackedAttn& a, int id, int& row0,
   int nth;
   if (!find_slot<false>(a, PACKED_BM, id, nth, s)) return false;
   row0 = ((s.lq * a.G + PACKED_BM - 1) / PACKED_BM - 1 - nth) * PACKED_BM;
-  return row0 >= 0;
+  return true;
 }
 
 // delta[head][token] = <dO, O>, from the rows as they are stored: LR lanes hold a row in 16-byte pieces.  (O's rounding is an error of
@@ -66,7 +66,6 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
   SeqGeom s;
   if (!find_slot<true>(a, KB, slot, nth, s)) return;
   const int k0 = nth * KB;
-  if (k0 >= s.lk) return;
   const int off = s.lk - s.lq, rows = s.lq * a.G, key = k0 + wave * 32 + r;
   frag_t<T> kf[NKD], vf[DK ? NKD : 1];
   {
@@ -215,7 +214,6 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
   SeqGeom s;
   if (!key_tile(b, slot_, nth, slot, s)) return;
   const int k0 = nth * KB;
-  if (k0 >= s.lk) return;
   const int off = s.lk - s.lq, rows = s.lq * a.G;
   const int first = a.causal ? max(k0 - off, 0) * a.G / QT * QT : 0;   // the first row tile that sees one of the keys
   // this range of the rows, and whether it is the only one
@@ -446,7 +444,6 @@ __global__ __launch_bounds__(512) void packed_dkv_join_kernel(PackedAttnBwd b) {
   SeqGeom s;
   if (!find_slot<true>(a, PACKED_KB, slot, nth, s)) return;
   const int k0 = nth * PACKED_KB;
-  if (k0 >= s.lk) return;
   const int off = s.lk - s.lq, rows = s.lq * a.G, first = a.causal ? max(k0 - off, 0) * a.G / PACKED_QT * PACKED_QT : 0;
   const int p0 = min(first, max(rows - 1, 0)) / b.rchunk, p1 = max(rows - 1, 0) / b.rchunk;
   if (p0 == p1) return;

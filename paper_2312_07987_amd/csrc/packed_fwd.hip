@@ -53,7 +53,7 @@ __global__ __launch_bounds__(512, 1) void packed_fwd_long_kernel(PackedAttn a) {
     row0 = ((s.lq * a.G + BM - 1) / BM - 1 - nth) * BM;
   }
   const int rows = s.lq * a.G;
-  if (row0 < 0 || row0 >= rows) return;
+  if (row0 >= rows) return;
   const int off = s.lk - s.lq, wr = row0 + wave * 32, row = wr + r;
   const int wq_first = div_by(min(wr, rows - 1), a.g_inv) + off, wq_last = div_by(min(wr + 31, rows - 1), a.g_inv) + off;
   const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv);

@@ -1,0 +1,72 @@
+"""Calls of the attention and norm operators at the edges of what their description allows, on the GPU: offsets that lie, unusual numbering of the
+work, scales, padding."""
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2312_07987_amd import binding
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+class Guarded:
+    """A tensor in the middle of a larger one that holds 5."""
+
+    def __init__(self, shape, dtype, pad=40):
+        self.all = torch.full((shape[0] + 2 * pad,) + tuple(shape[1:]), 5.0, dtype=dtype, device="cuda")
+        self.pad, self.t = pad, self.all[pad:pad + shape[0]]
+
+    def check(self):
+        assert torch.all(self.all[:self.pad] == 5.0) and torch.all(self.all[self.pad + self.t.shape[0]:] == 5.0)
+
+
+LYING = [
+    [0, 1152, 0, 1152],                                   # the second sequence's slots lie behind the third's
+    [1152, 700, 300, 0], [0, 0, 0, 1152], [500, 2000000000, -2000000000, 600], [1152, 0, 1152, 0], [-5, 10, 2000, 3],
+    [(i * 397) % 1153 for i in range(140)],               # more sequences than one probe tells apart
+]
+
+
+@pytest.mark.parametrize("dtype,H,Hk,d", [("bf16", 4, 2, 64), ("f32", 4, 2, 32), ("bf16", 2, 1, 128), ("bf16", 2, 2, 256)])
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("most", [1152, 1])
+def test_falling_offsets_stay_inside(dtype, H, Hk, d, causal, most):
+    """Whatever the offsets hold, forward and backward end, and touch nothing outside the tensors.  most 1: single tokens, keys in chunks."""
+    n = 1152
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rnd = lambda h: torch.randn(n, h, d, generator=g, device="cuda").to(DT[dtype])
+    q, k, v, dO = rnd(H), rnd(Hk), rnd(Hk), rnd(H)
+    for off in LYING:
+        print(off[:4], flush=True)
+        O, dQ, dK, dV = (Guarded((n, h, d), DT[dtype]) for h in (H, H, Hk, Hk))
+        lse = torch.full((H + 2, n), 5.0, device="cuda")
+        plan = binding.make_attention(q, k, v, O.t, len(off) - 1, most, n, causal)
+        ws = torch.zeros(max(binding.switchhead_attention_workspace_bytes(plan, b) for b in (False, True)), dtype=torch.uint8, device="cuda")
+        binding.switchhead_attention_forward(plan, q, k, v, i32(off), i32(off), O.t, lse[1:-1], ws)
+        torch.cuda.synchronize()
+        binding.switchhead_attention_backward(plan, q, k, v, O.t, dO, lse[1:-1], i32(off), i32(off), dQ.t, dK.t, dV.t, ws)
+        torch.cuda.synchronize()
+        for t in (O, dQ, dK, dV):
+            t.check()
+        assert torch.all(lse[0] == 5.0) and torch.all(lse[-1] == 5.0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_falling_offsets_behind_a_prefix(dtype):
+    n, H, Hk, d = 1152, 4, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda rows, h: torch.randn(rows, h, d, generator=g, device="cuda").to(DT[dtype])
+    q, k, kp = rnd(n, H), rnd(n, Hk), rnd(700, Hk)
+    for most in (1, 200, n):
+        for off in LYING:
+            print(most, off[:4], flush=True)
+            O = Guarded((n, H, d), DT[dtype])
+            plan = binding.make_attention(q, k, k, O.t, len(off) - 1, most, n, 1, kp, kp)
+            ws = torch.zeros(binding.switchhead_attention_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+            binding.switchhead_attention_forward(plan, q, k, k, i32(off), i32(off), O.t, None, ws, K_prefix=kp, V_prefix=kp)
+            torch.cuda.synchronize()
+            O.check()
