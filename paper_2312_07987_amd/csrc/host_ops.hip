@@ -286,6 +286,10 @@ PackedAttn packed_args(const AttnPlan& p, const int32_t* qoff, const int32_t* ql
 }
 
 // ---- norms ----------------------------------------------------------------------------------------------------------------
+// An output over its input: every element must lie where it lay (strides along one row or one head mean nothing)
+bool same_places(int64_t tokens, int64_t heads, int64_t row0, int64_t head0, int64_t row1, int64_t head1) {
+  return (tokens <= 1 || row0 == row1) && (heads <= 1 || head0 == head1);
+}
 sh_status plan_norm(sh_qk_norm& a, const sh_qk_norm* d) {
   if (!d) return fail(SH_ERR_INVALID_ARG, "the norms' description is NULL");
   a = *d;
@@ -476,7 +480,8 @@ sh_status switchhead_qk_norm_rope_forward(const sh_qk_norm* d, const void* Q, co
   if (!elements_aligned({Q, K, w_Q, w_K, Y_Q, Y_K}, esz) || !elements_aligned({positions}, 4)) return fail(SH_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if (!disjoint(a.tokens, a.nheads, a.yq_row, a.yq_head, a.d_head) || (a.nkv_heads && !disjoint(a.tokens, a.nkv_heads, a.yk_row, a.yk_head, a.d_head)))
     return fail(SH_ERR_INVALID_ARG, "the strides of Y_Q or Y_K lay rows over each other");
-  if ((Q == Y_Q && a.tokens > 1 && (a.q_row != a.yq_row || a.q_head != a.yq_head)) || (a.nkv_heads && K == Y_K && a.tokens > 1 && (a.k_row != a.yk_row || a.k_head != a.yk_head)))
+  if ((Q == Y_Q && !same_places(a.tokens, a.nheads, a.q_row, a.q_head, a.yq_row, a.yq_head)) ||
+      (a.nkv_heads && K == Y_K && !same_places(a.tokens, a.nkv_heads, a.k_row, a.k_head, a.yk_row, a.yk_head)))
     return fail(SH_ERR_INVALID_ARG, "an output over its input needs the input's strides");
   if (a.tokens == 0) return SH_OK;
   QkNormArgs n = norm_args(a, Q, K, w_Q, w_K, positions);
@@ -501,7 +506,8 @@ sh_status switchhead_qk_norm_rope_backward(const sh_qk_norm* d, const void* Q, c
     return fail(SH_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if (!disjoint(a.tokens, a.nheads, a.q_row, a.q_head, a.d_head) || (a.nkv_heads && !disjoint(a.tokens, a.nkv_heads, a.k_row, a.k_head, a.d_head)))
     return fail(SH_ERR_INVALID_ARG, "the strides of Q or K lay the rows of a gradient over each other");
-  if ((dQ == dY_Q && a.tokens > 1 && (a.q_row != a.yq_row || a.q_head != a.yq_head)) || (a.nkv_heads && dK == dY_K && a.tokens > 1 && (a.k_row != a.yk_row || a.k_head != a.yk_head)))
+  if ((dQ == dY_Q && !same_places(a.tokens, a.nheads, a.q_row, a.q_head, a.yq_row, a.yq_head)) ||
+      (a.nkv_heads && dK == dY_K && !same_places(a.tokens, a.nkv_heads, a.k_row, a.k_head, a.yk_row, a.yk_head)))
     return fail(SH_ERR_INVALID_ARG, "a gradient over its upstream gradient needs the same strides");
   if ((r = check_workspace(workspace, workspace_bytes, norm_bytes(a))) != SH_OK) return r;
   const hipStream_t st = (hipStream_t)hip_stream;
