@@ -197,7 +197,7 @@ struct BwdPlan {
   size_t dkv, ds, total;   // ds 0: not kept
   int rchunk, rparts;
   long ds_ld, dkv_floats;
-  double blocks;           // of its largest launch
+  double threads;          // of its largest launch
 };
 constexpr size_t MAX_DS_BYTES = (size_t)2 << 30;
 BwdPlan plan_backward(const AttnPlan& p) {
@@ -234,7 +234,8 @@ BwdPlan plan_backward(const AttnPlan& p) {
   }
   const double kb = p.klevels ? (double)p.klevels * a.nseq : packed_slots(a.total_k, PACKED_KB, a.nseq);
   const double qb = p.levels128 ? (double)p.levels128 * a.nseq : packed_slots((long)a.total_q * p.G, PACKED_BM, a.nseq);
-  b.blocks = std::fmax(kb * b.rparts, std::fmax((double)packed_slots(a.total_k, PACKED_KB, a.nseq), qb)) * a.nkv_heads;
+  b.threads = 512. * std::fmax(kb * b.rparts, std::fmax((double)packed_slots(a.total_k, PACKED_KB, a.nseq), qb)) * a.nkv_heads;
+  b.threads = std::fmax(b.threads, (double)packed_delta_lanes(a.d_head, p.esz) * a.total_q * a.nheads + 256.);
   b.total = off;
   return b;
 }
@@ -430,8 +431,8 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
       !disjoint(s.total_k, s.nkv_heads, s.v_row, s.v_head, s.d_head))
     return fail(SH_ERR_INVALID_ARG, "the strides of Q, K or V lay the rows of a gradient over each other");
   const BwdPlan w = plan_backward(p);
-  if (512. * w.blocks >= MAX_THREADS)
-    return fail(SH_ERR_UNSUPPORTED, "too large: the work-groups of nseq=%d, total_q=%d, total_k=%d do not fit one launch", s.nseq, s.total_q, s.total_k);
+  if (w.threads >= MAX_THREADS)
+    return fail(SH_ERR_UNSUPPORTED, "too large: the work-groups of nseq=%d, total_q=%d, total_k=%d, nheads=%d do not fit one launch", s.nseq, s.total_q, s.total_k, s.nheads);
   if ((r = check_workspace(workspace, workspace_bytes, w.total)) != SH_OK) return r;
   if (s.nseq == 0 || (s.total_q == 0 && s.total_k == 0)) return SH_OK;
   const hipStream_t st = (hipStream_t)hip_stream;

@@ -391,6 +391,12 @@ void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta
 enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128, PACKED_QT = 64 };
 // head width that a work-group's tiles are laid out for
 static inline int packed_width(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
+// lanes that share a row of the backward pass' <dO, O>: 16 bytes each
+static inline int packed_delta_lanes(int dh, int esz) {
+  int l = 8;
+  while (l * 16 < dh * esz) l *= 2;
+  return l;
+}
 // slots of `rows` rows in tiles of bm over nseq sequences
 static inline long packed_slots(long rows, int bm, int nseq) { return rows / bm + nseq; }
 

@@ -684,12 +684,12 @@ static void launch_bwd_t(const PackedAttnBwd& b, int align, float* delta, hipStr
   const PackedAttn& a = b.f;
   prof_mark(s, "attention.delta");
   if (a.total_q > 0) {   // (keys without a query get zeros below)
-    constexpr int N = Elem<T>::PER;
-    if (a.dh <= 8 * N)
+    const int lanes = packed_delta_lanes(a.dh, sizeof(T));
+    if (lanes == 8)
       launch_delta<T, 8>(b, align, delta, s);
-    else if (a.dh <= 16 * N)
+    else if (lanes == 16)
       launch_delta<T, 16>(b, align, delta, s);
-    else if (a.dh <= 32 * N)
+    else if (lanes == 32)
       launch_delta<T, 32>(b, align, delta, s);
     else if constexpr (sizeof(T) == 4)
       launch_delta<T, 64>(b, align, delta, s);

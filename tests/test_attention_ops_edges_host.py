@@ -9,6 +9,21 @@ from paper_2312_07987_amd import binding as b
 P = 0x10000   # an address that is never read
 
 
+def attention_backward(a, ws=1 << 50, **over):
+    p = dict(Q=P, K=2 * P, V=3 * P, O=4 * P, dO=5 * P, lse=6 * P, qo=7 * P, ql=None, ko=7 * P, kl=None, dQ=8 * P, dK=9 * P, dV=10 * P, workspace=11 * P)
+    p.update(over)
+    return b.lib().switchhead_attention_backward(ctypes.byref(a), *p.values(), ws, None)
+
+
+@pytest.mark.parametrize("d_head,dtype,rows", [(64, b.SH_BF16, 1 << 29), (128, b.SH_BF16, 1 << 28), (65, b.SH_BF16, 1 << 28), (256, b.SH_F32, 1 << 26), (32, b.SH_F32, 1 << 29)])
+def test_rows_whose_dot_products_no_launch_holds(d_head, dtype, rows):
+    """Several lanes form a row's <dO, O>: 2^32 of them are refused before anything runs, a few less are not (the workspace is checked next)."""
+    a = b.sh_attention(nseq=1, nheads=64, nkv_heads=1, d_head=d_head, causal=1, dtype=dtype, total_q=rows // 64, total_k=8, max_q=8, max_k=8)
+    assert attention_backward(a) == b.SH_ERR_UNSUPPORTED
+    a.total_q -= 8
+    assert attention_backward(a, ws=0) == b.SH_ERR_WORKSPACE_TOO_SMALL
+
+
 def norm_forward(a, Q=P, Y=2 * P, K=None, YK=None):
     return b.lib().switchhead_qk_norm_rope_forward(ctypes.byref(a), Q, K, None, None, None, Y, YK, None)
 
