@@ -523,7 +523,7 @@ void wgrad(const Ctx& c, WgradArgs a, bool deterministic = true, bool zero = tru
 }
 
 // Norms and rotation of one side of a packed layer (0 queries, 1 keys): queries and keys have token counts of their own, so each is a call with one side.
-// Rows that belong to no sequence have position 0.
+// Rows that belong to no sequence have position -1 and take no part: where such a row is zeros and norm_eps is 0, 1 / sqrt(0) would reach the weights' gradients.
 QkNormArgs packed_norm(const Ctx& c, int side) {
   const PackedLayer& k = *c.pk;
   QkNormArgs n{};
@@ -535,6 +535,7 @@ QkNormArgs packed_norm(const Ctx& c, int side) {
   n.y[0] = k.norm ? c.p<void>(side ? k.kn : k.qn) : x;
   n.dy[0] = n.dx[0] = d;
   n.positions = c.p<int>(k.pos) + (side ? 0 : k.prefix);
+  n.gaps = 1;
   n.tokens = side ? c.N : c.Nq;
   n.H[0] = c.H;
   n.dh = c.dh;
@@ -998,7 +999,7 @@ static sh_status layer_forward(const sh_shape* shape, const PackedLayer* pk, con
   if (pk) {
     if (pk->norm || shape->rope) {
       prof_mark(c.st, "fwd.norm_rope");
-      if (shape->rope) launch_packed_positions(pk->p->offsets, pk->p->nseq, pk->p->max_len, shape->T, pk->prefix, c.p<int>(pk->pos), c.st);
+      launch_packed_positions(pk->p->offsets, pk->p->nseq, pk->p->max_len, shape->T, pk->prefix, c.p<int>(pk->pos), c.st);
       launch_layer_norm_rope(packed_norm(c, 0), c.bf16, false, c.st);
       launch_layer_norm_rope(packed_norm(c, 1), c.bf16, false, c.st);
     }

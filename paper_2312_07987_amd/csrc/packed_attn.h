@@ -357,6 +357,7 @@ struct QkNormArgs {
   const void* x[2];
   const void* w[2];        // [dh] or NULL: ones
   const int* positions;    // [tokens] or NULL: the token's index
+  int gaps;                // negative positions mark tokens that take no part: y and dx stay as they are, dw has nothing of them
   void* y[2];
   const void* dy[2];
   void* dx[2];
@@ -376,7 +377,7 @@ void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipSt
 // for the layer (one side, dense rows): rates and alignment are filled in
 void launch_layer_norm_rope(QkNormArgs a, int bf16, bool backward, hipStream_t s);
 size_t packed_norm_bytes(long tokens, int heads, int dh, int bf16);
-// pos[r] = r for the prefix' rows, prefix + the row's place in its sequence for the others, 0 for rows of no sequence
+// pos[r] = r for the prefix' rows, prefix + the row's place in its sequence for the others, -1 for rows of no sequence
 void launch_packed_positions(const int* offsets, int nseq, int max_len, int T, int prefix, int* pos, hipStream_t s);
 // zeros in the rows that belong to no sequence of up to three tensors (NULL: none)
 void launch_packed_clear(const int* offsets, int nseq, int max_len, int rows, int row_bytes, void* p0, void* p1, void* p2, hipStream_t s);

@@ -102,6 +102,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_fwd_kernel(QkNormArgs a) {
     uint4 next = load_row_piece<T, AL>(x_, d, a.dh);
     float cs[N / 2], sn[N / 2];
     const double pos = a.positions ? a.positions[t] : (double)t;
+    if (a.gaps && pos < 0.) continue;
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) turn_cos_sin(pos * c.rate[j], cs[j], sn[j]);
     for (int h = h0; h < h1; ++h, y_ += yh) {
@@ -148,6 +149,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNormArgs a) {
     uint4 nx = load_row_piece<T, AL>(x_, d, a.dh), nd = load_row_piece<T, AL>(dy_, d, a.dh);
     float cs[N / 2], sn[N / 2];
     const double pos = a.positions ? a.positions[t] : (double)t;
+    if (a.gaps && pos < 0.) continue;
 #pragma unroll
     for (int j = 0; j < N / 2; ++j) turn_cos_sin(pos * c.rate[j], cs[j], sn[j]);
     for (int h = h0; h < h1; ++h, dx_ += xh) {
@@ -289,7 +291,6 @@ void launch_qk_norm_rope(QkNormArgs a, int bf16, int align, bool backward, hipSt
 
 void launch_layer_norm_rope(QkNormArgs a, int bf16, bool backward, hipStream_t s) {
   for (int k = 0; k < 7; ++k) a.rate[k] = a.rope_dim ? pow(10000., -2. * (1 << k) / a.rope_dim) : 0.;
-  if (a.rope_dim == 0) a.positions = nullptr;
   const int esz = bf16 ? 2 : 4;
   const unsigned long bits = (unsigned long)a.dh * esz | (unsigned long)(uintptr_t)a.w[0];   // (the workspace's rows begin at multiples of 256)
   launch_qk_norm_rope(a, bf16, bits % 16 == 0 ? 16 : bf16 && bits % 8 == 0 ? 8 : esz, backward, s);
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(256) void packed_positions_kernel(const int* offset
   const int row = blockIdx.x * 256 + threadIdx.x;
   if (row >= T) return;
   const int at = row < prefix ? -1 : place_in_sequence(offsets, nseq, max_len, row - prefix);
-  pos[row] = row < prefix ? row : at < 0 ? 0 : prefix + at;
+  pos[row] = row < prefix ? row : at < 0 ? -1 : prefix + at;
 }
 
 // zeros in the rows of up to three tensors that belong to no sequence: a wave per row

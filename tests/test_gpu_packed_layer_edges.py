@@ -1,0 +1,74 @@
+"""The layer over packed sequences at the edges of what its description allows, on the GPU, against the float64 form and the bars of test_gpu_packed_layer."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+from paper_2312_07987_amd import binding
+from paper_2312_07987_amd.inputs import make_inputs
+from paper_2312_07987_amd.runner import DeviceLayer
+from test_gpu_packed_layer import BF, F32, NAMES, close, reference
+
+pytestmark = pytest.mark.gpu
+
+
+class PackedCall:
+    """A layer, its packing and its workspace on the GPU; forward() and backward() are the calls."""
+
+    def __init__(self, cfg, offsets, rows, norm, eps, host=None, seed=3):
+        self.cfg = dict(cfg, B=1, T=rows)
+        self.host = make_inputs(self.cfg, seed=seed) if host is None else host
+        self.layer = DeviceLayer(self.cfg, self.host)
+        d = cfg["d_head"]
+        g = torch.Generator().manual_seed(5)
+        self.w = [(1 + 0.2 * torch.randn(d, generator=g)).to(self.layer.tdtype) for _ in range(2)] if norm else None
+        self.offsets = torch.tensor(offsets, dtype=torch.int32, device="cuda")
+        self.packing = binding.make_packing(self.offsets, rows, *([v.cuda() for v in self.w] if norm else (None, None)), norm_eps=eps)
+        self.ws = torch.full((binding.switchhead_packed_workspace_bytes(self.layer.shape, self.packing),), 255, dtype=torch.uint8, device="cuda")
+        self.dn = [torch.empty(d, device="cuda") if norm else None for _ in range(2)]
+
+    def forward(self):
+        l, W = self.layer, self.layer.W
+        binding.switchhead_forward_packed(l.shape, self.packing, l.x, W["W_Q"], W["W_K"], W["W_V"], W["W_O"], W["W_S"], W["W_D"], l.b_S, l.b_D, l.y, self.ws)
+
+    def backward(self):
+        l, W, dW = self.layer, self.layer.W, self.layer.dW
+        binding.switchhead_backward_packed(l.shape, self.packing, l.x, W["W_Q"], W["W_K"], W["W_V"], W["W_O"], W["W_S"], W["W_D"], l.dy, self.ws, l.dx,
+                                           dW["W_Q"], dW["W_K"], dW["W_V"], dW["W_O"], dW["W_S"], dW["W_D"], l.db_S, l.db_D, *self.dn)
+
+    def results(self):
+        torch.cuda.synchronize()
+        l = self.layer
+        out = dict(y=l.y, dx=l.dx, **{"d" + n: l.dW[n] for n in NAMES})
+        return {n: t for n, t in dict(out, dq_norm=self.dn[0], dk_norm=self.dn[1]).items() if t is not None}
+
+
+@pytest.mark.parametrize("base", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rope", [0, 1])
+def test_padding_of_zeros_without_epsilon(base, rope):
+    """norm_eps 0 and padding rows of zeros, whose norm has no value: they give nothing all the same."""
+    cfg = dict(base, rope=rope)
+    rows, lead, lens = 100, 9, [40, 17]
+    at = slice(lead, lead + sum(lens))
+    host = make_inputs(dict(cfg, B=1, T=rows), seed=3)
+    for n in ("x", "dy"):
+        kept = host[n][:, at].copy()
+        host[n][:] = 0
+        host[n][:, at] = kept
+    p = PackedCall(cfg, [lead, lead + 40, lead + 57], rows, True, 0.0, host)
+    p.forward()
+    p.backward()
+    got = p.results()
+    t = {n: None if host.get(n) is None else torch.from_numpy(host[n][:, at] if n == "x" else host[n]).double().requires_grad_(True) for n in ("x",) + NAMES}
+    wn = [v.double().requires_grad_(True) for v in p.w]
+    y = reference(cfg, t, [0, 40, 57], 0, wn, 0.0)
+    y.backward(torch.from_numpy(host["dy"][0, at]).double())
+    for n in ("y", "dx"):
+        out = torch.ones(rows, dtype=torch.bool)
+        out[at] = False
+        assert torch.all(got[n][0][out.cuda()] == 0), n
+    close("y", got["y"][0, at], y, cfg["dtype"])
+    close("dx", got["dx"][:, at], t["x"].grad, cfg["dtype"])
+    for n in NAMES:
+        close("d" + n, got["d" + n], t[n].grad, cfg["dtype"])
+    close("dq_norm", got["dq_norm"], wn[0].grad, cfg["dtype"])
+    close("dk_norm", got["dk_norm"], wn[1].grad, cfg["dtype"])
