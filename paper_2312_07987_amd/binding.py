@@ -31,14 +31,23 @@ class sh_shape(ctypes.Structure):
                 ("B", "T", "d_model", "nheads", "d_head", "E", "k", "causal", "dtype", "qk_experts", "rope", "T_q")]
 
 
-class sh_attention(ctypes.Structure):
+class _Description(ctypes.Structure):
+    """`places`: what the fields say about the tensors, kept until a field changes."""
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name != "places":
+            self.__dict__.pop("places", None)
+
+
+class sh_attention(_Description):
     _fields_ = ([(n, ctypes.c_int32) for n in ("nseq", "nheads", "nkv_heads", "d_head", "causal", "dtype", "total_q", "total_k",
                                                "max_q", "max_k", "prefix")] + [("scale", ctypes.c_float)] +
                 [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "o_row", "o_head",
                                                "kp_row", "kp_head", "vp_row", "vp_head")])
 
 
-class sh_qk_norm(ctypes.Structure):
+class sh_qk_norm(_Description):
     _fields_ = ([(n, ctypes.c_int32) for n in ("tokens", "nheads", "nkv_heads", "d_head", "rope_dim", "dtype")] +
                 [("eps", ctypes.c_float), ("theta", ctypes.c_float)] +
                 [(n, ctypes.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "yq_row", "yq_head", "yk_row", "yk_head")])
@@ -213,6 +222,9 @@ def switchhead_profile_read(max_entries=64):
 
 
 # ---- operators beside the layer ---------------------------------------------------------------------------------------------
+# These calls compare every tensor with the description and the types that the library reads it by: a gradient with other strides than its
+# tensor's (torch.empty_like of a view of a fused projection is dense), 64-bit offsets (torch.cumsum's result) or a tensor on another device would otherwise be read, or
+# written past its end, as what it is not.
 def _addr(t):
     return None if t is None else t.data_ptr()
 
@@ -220,63 +232,142 @@ def _addr(t):
 _torch = None
 
 
-def _launch(fn, device, stream, *args):
-    """Calls fn(*args, stream) with `device` current: its current stream where none is given."""
+def _import_torch():
     global _torch
     if _torch is None:
         import torch
         _torch = torch
-    cuda = _torch.cuda
-    if device.type != "cuda":
+    return _torch
+
+
+def _launch(fn, device, stream, *args):
+    """Calls fn(*args, stream) with GPU `device` current (-1: the tensors are in host memory): its current stream where none is given."""
+    if device < 0:
         raise SwitchHeadError(SH_ERR_INVALID_ARG, "the tensors must be on a GPU")
-    here = cuda.current_device()
-    if device.index is not None and device.index != here:
-        with cuda.device(device):
-            return _check(fn(*args, cuda.current_stream().cuda_stream if stream is None else int(stream)))
-    if stream is None:
-        stream = _torch._C._cuda_getCurrentRawStream(here)
-    code = fn(*args, int(stream))
+    if device != _torch._C._cuda_getDevice():
+        with _torch.cuda.device(device):
+            return _check(fn(*args, _torch.cuda.current_stream().cuda_stream if stream is None else int(stream)))
+    code = fn(*args, _torch._C._cuda_getCurrentRawStream(device) if stream is None else int(stream))
     if code != SH_OK:
         _check(code)
 
 
+def _refuse(text, *args):
+    raise SwitchHeadError(SH_ERR_INVALID_ARG, text % args)
+
+
 def _dtype_code(t):
-    import torch
+    torch = _import_torch()
     codes = {torch.float32: SH_F32, torch.bfloat16: SH_BF16}
     if t.dtype not in codes:
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "tensors are float32 or bfloat16, not %s" % t.dtype)
+        _refuse("tensors are float32 or bfloat16, not %s", t.dtype)
     return codes[t.dtype]
 
 
 def _rows(name, t, like=None, heads=None):
     """Row and head stride of a [rows, heads, d_head] tensor, its rows' elements next to each other."""
     if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s must be [rows, heads, d_head] with the elements of a head next to each other" % name)
+        _refuse("%s must be [rows, heads, d_head] with the elements of a head next to each other", name)
     if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s has another type, device or head width" % name)
+        _refuse("%s has another type, device or head width", name)
     if heads is not None and t.shape[1] != heads:
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s has %d heads, not %d" % (name, t.shape[1], heads))
+        _refuse("%s has %d heads, not %d", name, t.shape[1], heads)
     rows, head = t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2], t.stride(1) if t.shape[1] > 1 else t.shape[2]
     if rows == 0 or head == 0:
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "%s is broadcast along its rows or heads" % name)
+        _refuse("%s is broadcast along its rows or heads", name)
     return rows, head
+
+
+def _place(rows, heads, d, row, head):
+    """Shape and strides that a description means by these fields."""
+    head = head or d
+    return (rows, heads, d), (row or heads * head, head, 1)
+
+
+def _attention_places(a):
+    """Shapes and strides of Q, K, V, O and the prefix, the storage type."""
+    try:
+        return a.places
+    except AttributeError:
+        pass
+    torch = _import_torch()
+    q, k, d = (a.total_q, a.nheads), (a.total_k, a.nkv_heads), a.d_head
+    a.places = (_place(*q, d, a.q_row, a.q_head), _place(*k, d, a.k_row, a.k_head), _place(*k, d, a.v_row, a.v_head), _place(*q, d, a.o_row, a.o_head),
+                _place(a.prefix, a.nkv_heads, d, a.kp_row, a.kp_head), _place(a.prefix, a.nkv_heads, d, a.vp_row, a.vp_head),
+                torch.bfloat16 if a.dtype == SH_BF16 else torch.float32)
+    return a.places
+
+
+def _norm_places(a):
+    try:
+        return a.places
+    except AttributeError:
+        pass
+    torch = _import_torch()
+    n, H, Hk, d = a.tokens, a.nheads, a.nkv_heads, a.d_head
+    a.places = (_place(n, H, d, a.q_row, a.q_head), _place(n, Hk, d, a.k_row, a.k_head), _place(n, H, d, a.yq_row, a.yq_head), _place(n, Hk, d, a.yk_row, a.yk_head),
+                torch.bfloat16 if a.dtype == SH_BF16 else torch.float32)
+    return a.places
+
+
+def _lies(name, t, place, dtype, device):
+    """t lies as the description says (strides along one row or one head mean nothing)."""
+    shape, stride = place
+    if t is None:   # (a tensor without rows may be missing)
+        if shape[0]:
+            _refuse("%s is missing", name)
+        return
+    if t.shape == shape and t.stride() == stride and t.dtype is dtype and t.get_device() == device:
+        return
+    if tuple(t.shape) != shape or t.dtype != dtype:
+        _refuse("%s is %s %s, the description says %s %s", name, tuple(t.shape), t.dtype, shape, dtype)
+    if t.get_device() != device:
+        _refuse("%s is on another device", name)
+    if 0 not in shape and any(n > 1 and a != b for n, a, b in zip(shape, t.stride(), stride)):
+        _refuse("%s has strides %s, the description says %s", name, t.stride(), stride)
+
+
+def _dense(name, t, dtype, least, device):
+    """t holds at least `least` elements of this type without gaps, or is None (the library refuses that where it must not be)."""
+    if t is None:
+        return
+    if t.dtype is not dtype or t.numel() < least or not t.is_contiguous() or t.get_device() != device:
+        _refuse("%s must be at least %d elements of %s without gaps on the tensors' device, not %s %s%s", name, least, dtype, tuple(t.shape), t.dtype,
+                "" if t.is_contiguous() else " with gaps")
+
+
+def _workspace(t, device):
+    if not t.is_contiguous() or t.get_device() != device:
+        _refuse("the workspace must be without gaps and on the tensors' device")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _lengths(a, device, q_offsets, q_lengths, k_offsets, k_lengths):
+    i32 = _torch.int32
+    _dense("q_offsets", q_offsets, i32, a.nseq + 1, device)
+    if k_offsets is not q_offsets:
+        _dense("k_offsets", k_offsets, i32, a.nseq + 1, device)
+    _dense("q_lengths", q_lengths, i32, a.nseq, device)
+    _dense("k_lengths", k_lengths, i32, a.nseq, device)
+    return _addr(q_offsets), _addr(q_lengths), _addr(k_offsets), _addr(k_lengths)
 
 
 def make_attention(Q, K, V, O, nseq, max_q, max_k, causal=1, K_prefix=None, V_prefix=None, scale=0.0):
     """The description of attention over these tensors: Q, O [total_q, nheads, d_head], K, V [total_k, nkv_heads, d_head], strided as they
-    are (views of a fused projection, slices of a cache).  Valid for any tensors of the same shapes and strides."""
+    are (views of a fused projection, slices of a cache).  Valid for any tensors of the same shapes and strides; gradients have the strides of their tensors."""
     q, k, v, o = _rows("Q", Q), _rows("K", K, Q), _rows("V", V, Q, K.shape[1]), _rows("O", O, Q, Q.shape[1])
     if V.shape[0] != K.shape[0] or O.shape[0] != Q.shape[0]:
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "K and V, and Q and O, must have the same number of rows")
+        _refuse("K and V, and Q and O, must have the same number of rows")
     if (K_prefix is None) != (V_prefix is None):
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "K_prefix and V_prefix come together")
+        _refuse("K_prefix and V_prefix come together")
     prefix, kp, vp = 0, (0, 0), (0, 0)
     if K_prefix is not None:
         kp, vp, prefix = _rows("K_prefix", K_prefix, Q, K.shape[1]), _rows("V_prefix", V_prefix, Q, K.shape[1]), K_prefix.shape[0]
         if V_prefix.shape[0] != prefix:
-            raise SwitchHeadError(SH_ERR_INVALID_ARG, "K_prefix and V_prefix must have the same number of rows")
-    return sh_attention(nseq, Q.shape[1], K.shape[1], Q.shape[2], int(causal), _dtype_code(Q), Q.shape[0], K.shape[0], max_q, max_k, prefix,
-                        scale, *q, *k, *v, *o, *kp, *vp)
+            _refuse("K_prefix and V_prefix must have the same number of rows")
+    a = sh_attention(nseq, Q.shape[1], K.shape[1], Q.shape[2], int(causal), _dtype_code(Q), Q.shape[0], K.shape[0], max_q, max_k, prefix,
+                     scale, *q, *k, *v, *o, *kp, *vp)
+    return a
 
 
 def switchhead_attention_workspace_bytes(attention, backward=False):
@@ -285,49 +376,102 @@ def switchhead_attention_workspace_bytes(attention, backward=False):
 
 def switchhead_attention_forward(attention, Q, K, V, q_offsets, k_offsets, O, lse, workspace, q_lengths=None, k_lengths=None,
                                  K_prefix=None, V_prefix=None, stream=None):
-    _launch(lib().switchhead_attention_forward, Q.device, stream, attention, _addr(Q), _addr(K), _addr(V), _addr(K_prefix), _addr(V_prefix),
-            _addr(q_offsets), _addr(q_lengths), _addr(k_offsets), _addr(k_lengths), _addr(O), _addr(lse),
-            _addr(workspace), workspace.numel() * workspace.element_size())
+    q, k, v, o, kp, vp, dtype = _attention_places(attention)
+    device = Q.get_device()
+    _lies("Q", Q, q, dtype, device)
+    _lies("K", K, k, dtype, device)
+    _lies("V", V, v, dtype, device)
+    _lies("O", O, o, dtype, device)
+    if attention.prefix:
+        _lies("K_prefix", K_prefix, kp, dtype, device)
+        _lies("V_prefix", V_prefix, vp, dtype, device)
+    _dense("lse", lse, _torch.float32, attention.nheads * attention.total_q, device)
+    lengths = _lengths(attention, device, q_offsets, q_lengths, k_offsets, k_lengths)
+    _launch(lib().switchhead_attention_forward, device, stream, attention, _addr(Q), _addr(K), _addr(V), _addr(K_prefix), _addr(V_prefix),
+            *lengths, _addr(O), _addr(lse), *_workspace(workspace, device))
 
 
 def switchhead_attention_backward(attention, Q, K, V, O, dO, lse, q_offsets, k_offsets, dQ, dK, dV, workspace, q_lengths=None,
                                   k_lengths=None, stream=None):
-    _launch(lib().switchhead_attention_backward, Q.device, stream, attention, _addr(Q), _addr(K), _addr(V), _addr(O), _addr(dO), _addr(lse),
-            _addr(q_offsets), _addr(q_lengths), _addr(k_offsets), _addr(k_lengths), _addr(dQ), _addr(dK), _addr(dV),
-            _addr(workspace), workspace.numel() * workspace.element_size())
+    q, k, v, o, _, _, dtype = _attention_places(attention)
+    device = Q.get_device()
+    for name, t, place in (("Q", Q, q), ("K", K, k), ("V", V, v), ("O", O, o), ("dO", dO, o), ("dQ", dQ, q), ("dK", dK, k), ("dV", dV, v)):
+        _lies(name, t, place, dtype, device)
+    _dense("lse", lse, _torch.float32, attention.nheads * attention.total_q, device)
+    lengths = _lengths(attention, device, q_offsets, q_lengths, k_offsets, k_lengths)
+    _launch(lib().switchhead_attention_backward, device, stream, attention, _addr(Q), _addr(K), _addr(V), _addr(O), _addr(dO),
+            _addr(lse), *lengths, _addr(dQ), _addr(dK), _addr(dV), *_workspace(workspace, device))
 
 
 def make_qk_norm(Q, K, Y_Q, Y_K, rope_dim, eps=1e-6, theta=0.0):
-    """The description of norms and rotation of these tensors, [tokens, heads, d_head] each; K and Y_K may be None."""
+    """The description of norms and rotation of these tensors, [tokens, heads, d_head] each; K and Y_K may be None.  Valid for any tensors of the same
+    shapes and strides; gradients have the strides of their tensors."""
     q, yq = _rows("Q", Q), _rows("Y_Q", Y_Q, Q, Q.shape[1])
     if Y_Q.shape[0] != Q.shape[0] or (K is None) != (Y_K is None) or (K is not None and (K.shape[0] != Q.shape[0] or Y_K.shape[0] != Q.shape[0])):
-        raise SwitchHeadError(SH_ERR_INVALID_ARG, "Q, K and the outputs must have the same number of rows")
+        _refuse("Q, K and the outputs must have the same number of rows")
     k, yk, kv = (0, 0), (0, 0), 0
     if K is not None:
         k, yk, kv = _rows("K", K, Q), _rows("Y_K", Y_K, Q, K.shape[1]), K.shape[1]
-    return sh_qk_norm(Q.shape[0], Q.shape[1], kv, Q.shape[2], rope_dim, _dtype_code(Q), eps, theta, *q, *k, *yq, *yk)
+    a = sh_qk_norm(Q.shape[0], Q.shape[1], kv, Q.shape[2], rope_dim, _dtype_code(Q), eps, theta, *q, *k, *yq, *yk)
+    return a
 
 
 def switchhead_qk_norm_workspace_bytes(norm):
     return int(lib().switchhead_qk_norm_workspace_bytes(norm))
 
 
+def _norm_inputs(norm, Q, K, w_Q, w_K, positions, q, k, dtype, device):
+    _lies("Q", Q, q, dtype, device)
+    if norm.nkv_heads:
+        _lies("K", K, k, dtype, device)
+    _dense("w_Q", w_Q, dtype, norm.d_head, device)
+    _dense("w_K", w_K, dtype, norm.d_head, device)
+    _dense("positions", positions, _torch.int32, norm.tokens, device)
+
+
 def switchhead_qk_norm_rope_forward(norm, Q, K, w_Q, w_K, positions, Y_Q, Y_K, stream=None):
-    _launch(lib().switchhead_qk_norm_rope_forward, Q.device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
+    q, k, yq, yk, dtype = _norm_places(norm)
+    device = Q.get_device()
+    _norm_inputs(norm, Q, K, w_Q, w_K, positions, q, k, dtype, device)
+    _lies("Y_Q", Y_Q, yq, dtype, device)
+    if norm.nkv_heads:
+        _lies("Y_K", Y_K, yk, dtype, device)
+    _launch(lib().switchhead_qk_norm_rope_forward, device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
             _addr(Y_Q), _addr(Y_K))
 
 
 def switchhead_qk_norm_rope_backward(norm, Q, K, w_Q, w_K, positions, dY_Q, dY_K, dQ, dK, dw_Q, dw_K, workspace, stream=None):
-    _launch(lib().switchhead_qk_norm_rope_backward, Q.device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
-            _addr(dY_Q), _addr(dY_K), _addr(dQ), _addr(dK), _addr(dw_Q), _addr(dw_K),
-            _addr(workspace), workspace.numel() * workspace.element_size())
+    q, k, yq, yk, dtype = _norm_places(norm)
+    device = Q.get_device()
+    _norm_inputs(norm, Q, K, w_Q, w_K, positions, q, k, dtype, device)
+    _lies("dY_Q", dY_Q, yq, dtype, device)
+    _lies("dQ", dQ, q, dtype, device)
+    if norm.nkv_heads:
+        _lies("dY_K", dY_K, yk, dtype, device)
+        _lies("dK", dK, k, dtype, device)
+    _dense("dw_Q", dw_Q, _torch.float32, norm.d_head, device)
+    _dense("dw_K", dw_K, _torch.float32, norm.d_head, device)
+    _launch(lib().switchhead_qk_norm_rope_backward, device, stream, norm, _addr(Q), _addr(K), _addr(w_Q), _addr(w_K), _addr(positions),
+            _addr(dY_Q), _addr(dY_K), _addr(dQ), _addr(dK), _addr(dw_Q), _addr(dw_K), *_workspace(workspace, device))
 
 
 def make_packing(offsets, max_len, q_norm=None, k_norm=None, norm_eps=1e-6):
-    """Packed sequences of a layer call: offsets int32 [nseq + 1] on the GPU (kept alive by the packing), weights of the norms or None."""
+    """Packed sequences of a layer call: offsets int32 [nseq + 1] on the GPU, weights of the norms or None (all kept alive by the packing)."""
+    _dense("offsets", offsets, _import_torch().int32, 2, offsets.get_device())
     p = sh_packing(offsets.numel() - 1, max_len, _addr(offsets), _addr(q_norm), _addr(k_norm), norm_eps)
     p.tensors = (offsets, q_norm, k_norm)
     return p
+
+
+def _packing_fits(packing, shape, x, *gradients):
+    torch, device = _import_torch(), x.get_device()
+    offsets, q_norm, k_norm = getattr(packing, "tensors", (None, None, None))
+    _dense("offsets", offsets, torch.int32, packing.nseq + 1, device)
+    for t in (q_norm, k_norm):
+        _dense("a norm's weights", t, torch.bfloat16 if shape.dtype == SH_BF16 else torch.float32, shape.d_head, device)
+    for t in gradients:
+        _dense("a norm's gradient", t, torch.float32, shape.d_head, device)
+    return device
 
 
 def switchhead_packed_workspace_bytes(shape, packing):
@@ -335,12 +479,14 @@ def switchhead_packed_workspace_bytes(shape, packing):
 
 
 def switchhead_forward_packed(shape, packing, x, W_Q, W_K, W_V, W_O, W_S, W_D, b_S, b_D, y, workspace, stream=None):
-    _launch(lib().switchhead_forward_packed, x.device, stream, shape, packing, _addr(x), _addr(W_Q), _addr(W_K), _addr(W_V), _addr(W_O),
-            _addr(W_S), _addr(W_D), _addr(b_S), _addr(b_D), _addr(y), _addr(workspace), workspace.numel() * workspace.element_size())
+    device = _packing_fits(packing, shape, x)
+    _launch(lib().switchhead_forward_packed, device, stream, shape, packing, _addr(x), _addr(W_Q), _addr(W_K), _addr(W_V), _addr(W_O),
+            _addr(W_S), _addr(W_D), _addr(b_S), _addr(b_D), _addr(y), *_workspace(workspace, device))
 
 
 def switchhead_backward_packed(shape, packing, x, W_Q, W_K, W_V, W_O, W_S, W_D, dy, workspace, dx, dW_Q, dW_K, dW_V, dW_O, dW_S, dW_D, db_S, db_D,
                                dq_norm=None, dk_norm=None, stream=None):
-    _launch(lib().switchhead_backward_packed, x.device, stream, shape, packing, _addr(x), _addr(W_Q), _addr(W_K), _addr(W_V), _addr(W_O),
-            _addr(W_S), _addr(W_D), _addr(dy), _addr(workspace), workspace.numel() * workspace.element_size(), _addr(dx), _addr(dW_Q),
+    device = _packing_fits(packing, shape, x, dq_norm, dk_norm)
+    _launch(lib().switchhead_backward_packed, device, stream, shape, packing, _addr(x), _addr(W_Q), _addr(W_K), _addr(W_V), _addr(W_O),
+            _addr(W_S), _addr(W_D), _addr(dy), *_workspace(workspace, device), _addr(dx), _addr(dW_Q),
             _addr(dW_K), _addr(dW_V), _addr(dW_O), _addr(dW_S), _addr(dW_D), _addr(db_S), _addr(db_D), _addr(dq_norm), _addr(dk_norm))
