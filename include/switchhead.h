@@ -305,7 +305,8 @@ sh_status switchhead_attention_forward(const sh_attention* a, const void* Q, con
                                        void* O, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Gradients of <O, dO>: O and lse as forward left them (same description, prefix 0).  dK, dV sum over the query heads of their kv head.
- * Rows of sequences are overwritten, other rows left.  Deterministic: no atomics. */
+ * Rows of sequences are overwritten, other rows left.  Deterministic: no atomics.  The gradients may lie over no input and not over each other (views of one
+ * buffer whose rows alternate are fine). */
 sh_status switchhead_attention_backward(const sh_attention* a, const void* Q, const void* K, const void* V,
                                         const void* O, const void* dO, const float* lse,
                                         const int32_t* q_offsets, const int32_t* q_lengths,
@@ -318,7 +319,7 @@ sh_status switchhead_attention_backward(const sh_attention* a, const void* Q, co
  *   n = x w / sqrt(mean(x^2) + eps)  over the d_head elements of a row and head,  y = n with each pair (2i, 2i + 1), 2i < rope_dim,
  *   turned by positions[token] * theta^(-2i / rope_dim)
  * (the rotation of sh_shape::rope; rope_dim 0: none).  Q -> Y_Q [tokens, nheads, d_head], K -> Y_K [tokens, nkv_heads, d_head],
- * strides in elements, 0 = dense; nkv_heads 0: queries only, K may be NULL.  Y may be the input itself (same strides).  w_Q, w_K: [d_head]
+ * strides in elements, 0 = dense; nkv_heads 0: queries only, K may be NULL.  Y may be its own input (same strides), and overlaps nothing else.  w_Q, w_K: [d_head]
  * in storage type, shared by the heads, or NULL for ones.  positions: int32 [tokens] on the device (any value), or NULL: 0, 1, 2, ...
  */
 typedef struct {

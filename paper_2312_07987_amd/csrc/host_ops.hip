@@ -43,6 +43,13 @@ bool elements_aligned(std::initializer_list<const void*> ptrs, int esz) {
   return true;
 }
 
+bool any_same(std::initializer_list<const void*> outs, std::initializer_list<const void*> ins) {
+  for (const void* o : outs)
+    for (const void* i : ins)
+      if (o && o == i) return true;
+  return false;
+}
+
 // Rows of a tensor [rows, heads, d] in memory: dense where the strides are 0.  Limits: a tile's rows are addressed by 32-bit byte offsets.
 bool fill_strides(int64_t& row, int64_t& head, int64_t heads, int64_t d) {
   if (row < 0 || head < 0) return false;
@@ -366,6 +373,7 @@ sh_status switchhead_attention_forward(const sh_attention* d, const void* Q, con
     return fail(SH_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if ((r = check_workspace(workspace, workspace_bytes, p.total)) != SH_OK) return r;
   if (s.nseq == 0 || s.total_q == 0 || s.max_q == 0) return SH_OK;
+  if (any_same({O}, {K, V, K_prefix, V_prefix})) return fail(SH_ERR_INVALID_ARG, "O lies over keys or values");
   const hipStream_t st = (hipStream_t)hip_stream;
   const int bf16 = s.dtype == SH_BF16;
   const int align = alignment({Q, K, V, O, K_prefix, V_prefix}, {s.q_row, s.q_head, s.k_row, s.k_head, s.v_row, s.v_head, s.o_row, s.o_head, s.kp_row, s.kp_head, s.vp_row, s.vp_head},
@@ -435,6 +443,10 @@ sh_status switchhead_attention_backward(const sh_attention* d, const void* Q, co
     return fail(SH_ERR_UNSUPPORTED, "too large: the work-groups of nseq=%d, total_q=%d, total_k=%d, nheads=%d do not fit one launch", s.nseq, s.total_q, s.total_k, s.nheads);
   if ((r = check_workspace(workspace, workspace_bytes, w.total)) != SH_OK) return r;
   if (s.nseq == 0 || (s.total_q == 0 && s.total_k == 0)) return SH_OK;
+  // dK and dV are written before dQ reads K (and, where score gradients are not kept, Q, V and dO), and by other work-groups than those that still read
+  const void *const oq = s.total_q ? dQ : nullptr, *const ok = s.total_k ? dK : nullptr, *const ov = s.total_k ? dV : nullptr;
+  if (any_same({ok, ov}, {Q, K, V, dO}) || any_same({oq}, {K, V, ok, ov}) || any_same({ok}, {ov}))
+    return fail(SH_ERR_INVALID_ARG, "a gradient lies over a tensor that is still read, or over another gradient");
   const hipStream_t st = (hipStream_t)hip_stream;
   const int bf16 = s.dtype == SH_BF16;
   const int align = alignment({Q, K, V, O, dO, dQ, dK, dV}, {s.q_row, s.q_head, s.k_row, s.k_head, s.v_row, s.v_head, s.o_row, s.o_head}, s.d_head, p.esz);
@@ -485,6 +497,7 @@ sh_status switchhead_qk_norm_rope_forward(const sh_qk_norm* d, const void* Q, co
       (a.nkv_heads && K == Y_K && !same_places(a.tokens, a.nkv_heads, a.k_row, a.k_head, a.yk_row, a.yk_head)))
     return fail(SH_ERR_INVALID_ARG, "an output over its input needs the input's strides");
   if (a.tokens == 0) return SH_OK;
+  if (a.nkv_heads && (any_same({Y_Q}, {K, Y_K}) || any_same({Y_K}, {Q}))) return fail(SH_ERR_INVALID_ARG, "Y_Q or Y_K lies over the other side's tensor");
   QkNormArgs n = norm_args(a, Q, K, w_Q, w_K, positions);
   n.y[0] = Y_Q;
   n.y[1] = Y_K;
@@ -517,6 +530,7 @@ sh_status switchhead_qk_norm_rope_backward(const sh_qk_norm* d, const void* Q, c
     if (dw_K) launch_fill_f32(dw_K, a.d_head, 0.f, st);
     return check_launch("switchhead_qk_norm_rope_backward");
   }
+  if (a.nkv_heads && (any_same({dQ}, {K, dY_K, dK}) || any_same({dK}, {Q, dY_Q}))) return fail(SH_ERR_INVALID_ARG, "dQ or dK lies over the other side's tensor");
   QkNormArgs n = norm_args(a, Q, K, w_Q, w_K, positions);
   n.dy[0] = dY_Q;
   n.dy[1] = dY_K;

@@ -45,6 +45,23 @@ def test_one_token_in_place_needs_the_same_head_strides():
     assert norm_backward(a, dQ=2 * P) == b.SH_ERR_INVALID_ARG
 
 
+def test_outputs_over_what_is_still_read():
+    """Refused where the addresses say so: dK and dV are written before dQ's kernel reads K (and the rest, where it works the scores out again)."""
+    a = b.sh_attention(nseq=1, nheads=4, nkv_heads=4, d_head=64, causal=1, dtype=b.SH_BF16, total_q=10, total_k=10, max_q=10, max_k=10)
+    for out, at in (("dK", 1), ("dK", 2), ("dK", 3), ("dK", 5), ("dV", 1), ("dV", 2), ("dV", 3), ("dV", 5), ("dQ", 2), ("dQ", 3), ("dQ", 9), ("dQ", 10), ("dV", 9)):
+        assert attention_backward(a, **{out: at * P}) == b.SH_ERR_INVALID_ARG, (out, at)
+    assert b"gradient" in b.lib().switchhead_last_error()
+    for at in (2, 3, 5, 6):
+        p = dict(Q=P, K=2 * P, V=3 * P, KP=5 * P, VP=6 * P, qo=7 * P, ql=None, ko=7 * P, kl=None, O=at * P, lse=None, workspace=11 * P)
+        a.prefix = 3
+        assert b.lib().switchhead_attention_forward(ctypes.byref(a), *p.values(), 1 << 40, None) == b.SH_ERR_INVALID_ARG
+    n = b.sh_qk_norm(tokens=4, nheads=2, nkv_heads=2, d_head=64, rope_dim=0, dtype=b.SH_BF16)
+    for Y, YK in ((3 * P, 4 * P), (2 * P, P), (2 * P, 2 * P)):
+        assert norm_forward(n, Q=P, K=3 * P, Y=Y, YK=YK) == b.SH_ERR_INVALID_ARG
+    for dQ, dK in ((5 * P, 8 * P), (6 * P, 8 * P), (8 * P, P), (8 * P, 2 * P), (8 * P, 8 * P)):
+        assert norm_backward(n, K=5 * P, dYK=6 * P, dQ=dQ, dK=dK) == b.SH_ERR_INVALID_ARG
+
+
 # ---- the binding compares tensors with the description -----------------------------------------------------------------------
 def tensors(dtype="bfloat16"):
     torch = pytest.importorskip("torch")
