@@ -286,7 +286,7 @@ typedef struct {
   int32_t max_q, max_k;                /* no sequence has more queries, or own keys: further ones are treated as not
                                           there.  They size the grids and choose how work is split                   */
   int32_t prefix;                      /* rows of K_prefix, V_prefix [prefix, nkv_heads, d_head] that every query sees
-                                          in front of its own keys; 0: none                                          */
+                                          in front of its own keys, below 2^30; 0: none                              */
   float scale;                         /* > 0, or 0 for 1 / sqrt(d_head)                                             */
   int64_t q_row, q_head, k_row, k_head, v_row, v_head, o_row, o_head;
   int64_t kp_row, kp_head, vp_row, vp_head;   /* of K_prefix, V_prefix                                               */

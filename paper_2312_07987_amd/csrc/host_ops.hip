@@ -107,6 +107,7 @@ sh_status plan_attention(AttnPlan& p, const sh_attention* d) {
   const long G = p.G, rows = (long)a.total_q * G, most = (long)a.max_q * G;
   if ((long)a.total_q * a.nheads >= (1l << 31) || (long)a.total_k * G >= (1l << 31) - 128 * G || most * G >= (1l << 32) || a.nseq >= (1 << 24))
     return fail(SH_ERR_UNSUPPORTED, "too large: total_q * nheads and total_k * group must stay below 2^31, max_q * group^2 below 2^32, nseq below 2^24");
+  if (a.prefix >= 1 << 30) return fail(SH_ERR_UNSUPPORTED, "prefix=%d: must stay below 2^30", a.prefix);
 
   p.dhp = (a.d_head + 3) / 4 * 4;
   p.few = most <= PACKED_FEW;

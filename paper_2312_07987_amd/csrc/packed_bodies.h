@@ -69,7 +69,8 @@ __device__ __forceinline__ void packed_fwd_body(const PackedAttn& a, int b, type
 
   // tiles of the prefix, then of the own keys; this work-group's even share of them
   const int np = (prefix + KT - 1) / KT, nt = np + (kend + KT - 1) / KT;
-  const int t0 = (int)((unsigned)(nt * split) / (unsigned)ns), t1 = (int)((unsigned)(nt * (split + 1)) / (unsigned)ns);   // (below 2^25 tiles, 32 parts)
+  // (prefix below 2^30 rows, own keys below 2^31: less than 3 * 2^25 tiles, times up to 32 parts below 2^32)
+  const int t0 = (int)((unsigned)nt * (unsigned)split / (unsigned)ns), t1 = (int)((unsigned)nt * (unsigned)(split + 1) / (unsigned)ns);
   PieceTile<T, DH, AL, KT, 256> tk, tv;
   const raw* const KP = (const raw*)a.KP + (long)hk * a.kp_head;
   const raw* const VP = (const raw*)a.VP + (long)hk * a.vp_head;

@@ -62,6 +62,13 @@ def test_outputs_over_what_is_still_read():
         assert norm_backward(n, K=5 * P, dYK=6 * P, dQ=dQ, dK=dK) == b.SH_ERR_INVALID_ARG
 
 
+def test_prefix_whose_tiles_pass_32_bits():
+    a = b.sh_attention(nseq=1, nheads=1, nkv_heads=1, d_head=1, causal=1, dtype=b.SH_BF16, total_q=10, total_k=10, max_q=10, max_k=10, prefix=1 << 30)
+    assert b.switchhead_attention_workspace_bytes(a) == 0
+    a.prefix -= 1
+    assert b.switchhead_attention_workspace_bytes(a) > 0
+
+
 # ---- the binding compares tensors with the description -----------------------------------------------------------------------
 def tensors(dtype="bfloat16"):
     torch = pytest.importorskip("torch")
