@@ -1,9 +1,12 @@
 """Calls of the attention and norm operators at the edges of what their description allows, on the GPU: offsets that lie, unusual numbering of the
 work, scales, padding."""
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
 from paper_2312_07987_amd import binding
+from test_gpu_attention_ops import Packed
 
 pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -70,3 +73,39 @@ def test_falling_offsets_behind_a_prefix(dtype):
             binding.switchhead_attention_forward(plan, q, k, k, i32(off), i32(off), O.t, None, ws, K_prefix=kp, V_prefix=kp)
             torch.cuda.synchronize()
             O.check()
+
+
+def by_slot(lengths, group, kv_heads, tile=128):
+    """The sequences are so many and the longest so long that a launch under a causal mask numbers its tiles one sequence after the other, not by level."""
+    tiles = -(-max(lengths) * group // tile)
+    return tiles * len(lengths) > 2 * (sum(lengths) * group // tile + len(lengths)) + 1024 // kv_heads
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("H,Hk,d", [(4, 4, 64), (8, 8, 76), (4, 4, 128), (4, 2, 32)])
+@pytest.mark.parametrize("place", ["front", "middle", "end"])
+def test_a_long_document_among_many_short_ones(H, Hk, d, dtype, place):
+    """Causal training batches whose tiles, of rows and of keys, are numbered by slot."""
+    lens = [(i * 5) % 4 for i in range(300)]
+    lens.insert(dict(front=0, middle=150, end=300)[place], 700)
+    assert by_slot(lens, H // Hk, Hk) and by_slot(lens, 1, Hk)
+    Packed(H, Hk, d, dtype, lens, seed=40).check(backward=True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [0.02, 0.7])
+def test_a_scale_of_its_own(dtype, scale):
+    for p in (Packed(4, 2, 64, dtype, [40, 1, 130], seed=41), Packed(2, 1, 76, dtype, [60, 5], [90, 300], seed=42, causal=0)):
+        p.scale = scale
+        p.check(backward=True, scale=scale)
+    for p in (Packed(4, 2, 64, dtype, [1, 1], [700, 30], seed=43), Packed(4, 2, 64, dtype, [1, 5], [70, 30], prefix=900, seed=44)):
+        p.scale = scale
+        p.check(scale=scale)
+
+
+def test_gradients_when_every_key_is_visible_and_none_is_queried():
+    """Keys without queries get gradients of zero, queries without keys too; whole launches without rows on one side."""
+    for nq, nk in (([0, 0], [70, 5]), ([70, 5], [0, 0]), ([0, 3], [9, 0])):
+        for causal in (0, 1):
+            for dtype in ("f32", "bf16"):
+                Packed(4, 2, 64, dtype, nq, nk, causal=causal, seed=45).check(backward=True, max_q=max(max(nq), 1), max_k=max(max(nk), 1))

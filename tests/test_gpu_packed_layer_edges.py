@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
+from oracle import switchhead_oracle as orc
 from paper_2312_07987_amd import binding
 from paper_2312_07987_amd.inputs import make_inputs
 from paper_2312_07987_amd.runner import DeviceLayer
@@ -14,10 +15,10 @@ pytestmark = pytest.mark.gpu
 class PackedCall:
     """A layer, its packing and its workspace on the GPU; forward() and backward() are the calls."""
 
-    def __init__(self, cfg, offsets, rows, norm, eps, host=None, seed=3):
+    def __init__(self, cfg, offsets, rows, norm, eps, host=None, seed=3, dense=False):
         self.cfg = dict(cfg, B=1, T=rows)
         self.host = make_inputs(self.cfg, seed=seed) if host is None else host
-        self.layer = DeviceLayer(self.cfg, self.host)
+        self.layer = DeviceLayer(self.cfg, self.host, dense=dense)
         d = cfg["d_head"]
         g = torch.Generator().manual_seed(5)
         self.w = [(1 + 0.2 * torch.randn(d, generator=g)).to(self.layer.tdtype) for _ in range(2)] if norm else None
@@ -72,3 +73,61 @@ def test_padding_of_zeros_without_epsilon(base, rope):
         close("d" + n, got["d" + n], t[n].grad, cfg["dtype"])
     close("dq_norm", got["dq_norm"], wn[0].grad, cfg["dtype"])
     close("dk_norm", got["dk_norm"], wn[1].grad, cfg["dtype"])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind", ["experts for queries and keys", "one table for both sides", "dense", "biases"])
+def test_kinds_of_layers(kind, dtype):
+    """Every kind of the layer, packed, against the float64 oracle's plain layer called for one sequence after the other."""
+    cfg = dict(dict(F32) if dtype == "f32" else dict(BF), rope=1)
+    cfg.update({"experts for queries and keys": dict(qk_experts=1), "dense": dict(E=1, k=1), "biases": dict(bias0=0.5)}.get(kind, {}))
+    dense, lens, rows = kind == "dense", [70, 1, 33], 110
+    host = make_inputs(dict(cfg, B=1, T=rows), seed=11, shared_router=kind == "one table for both sides")
+    p = PackedCall(cfg, [0, 70, 71, 104], rows, False, 0.0, host, dense=dense)
+    p.forward()
+    p.backward()
+    got, sums, at = p.results(), {}, 0
+    y, dx = [], []
+    W = {n: None if dense and n in ("W_S", "W_D") else host[n] for n in NAMES}
+    for n in lens:
+        f = orc.forward(host["x"][:, at:at + n], *[W[m] for m in NAMES], host["b_S"], host["b_D"], k=cfg["k"], causal=True, rope=True, T_q=None)
+        g = orc.backward(host["x"][:, at:at + n], *[W[m] for m in NAMES], f, host["dy"][:, at:at + n])
+        y.append(torch.from_numpy(np.asarray(f["y"], dtype=np.float64)))
+        dx.append(torch.from_numpy(np.asarray(g["dx"], dtype=np.float64)))
+        for m in NAMES:
+            if W[m] is not None:
+                sums[m] = sums.get(m, 0) + np.asarray(g["d" + m], dtype=np.float64)
+        at += n
+    assert torch.all(got["y"][0, at:] == 0) and torch.all(got["dx"][0, at:] == 0)
+    close("y", got["y"][:, :at], torch.cat(y, 1), dtype)
+    close("dx", got["dx"][:, :at], torch.cat(dx, 1), dtype)
+    for m in sums:
+        close("d" + m, got["d" + m], torch.from_numpy(sums[m]), dtype)
+
+
+@pytest.mark.parametrize("base", [F32, BF], ids=["f32", "bf16"])
+def test_captured_and_replayed_with_other_lengths(base):
+    """A captured training step reads the offsets from the device: replays follow them, with other work between them."""
+    p = PackedCall(dict(base, rope=1), [0, 30, 90], 100, True, 1e-5)
+
+    def step():
+        p.forward()
+        p.backward()
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for offsets in ([0, 30, 90], [0, 1, 100], [10, 10, 60], [0, 30, 90]):
+        p.offsets.copy_(torch.tensor(offsets, dtype=torch.int32))
+        for t in p.results().values():
+            t.fill_(7.0)
+        graph.replay()
+        again = {n: t.clone() for n, t in p.results().items()}
+        step()
+        for n, t in p.results().items():
+            close(n, again[n], t.double().cpu(), "f32")   # (weight gradients may be added with fp32 atomics: not to the last bit)
