@@ -207,6 +207,16 @@ struct BwdPlan {
   long ds_ld, dkv_floats;
   double threads;          // of its largest launch
 };
+// Kept score gradients, for heads of 65 .. 128 elements, in up to 2 GiB.  A backward pass with them / with scores worked out again for dQ, us, 16 heads over 4 and
+// over 16:
+//   d    32 x 256 tokens        4 x 2048                 1 x 8192                   4096 and 20 of 300
+//   128  94 / 113, 128 / 139    353 / 380, 333 / 320     1287 / 1381, 1007 / 1030   597 / 663, 381 / 420
+//   96   79 / 87,  118 / 124    292 / 311, 298 / 267     1060 / 1124, 889 / 827     490 / 527, 343 / 333
+//   76   78 / 84,  122 / 134    314 / 334, 315 / 289     1162 / 1227, 959 / 882     547 / 584, 365 / 371
+//   64   66 / 68,   90 / 89     248 / 239, 232 / 194      932 / 857,  752 / 608     423 / 426, 295 / 269
+//   32   56 / 54,   75 / 74     222 / 207, 221 / 160      848 / 748,  728 / 495     376 / 384, 267 / 228
+// A pair of query and key costs its two bytes there and back whatever the width, but 8 d operations again: below 65 those are the cheaper ones.  The limit is
+// for the memory, which is laid out for the longest sequence: 4 x 4096 tokens of 32 heads of 128 over 8 would take 4 GiB for 2049 us against 2175.
 constexpr size_t MAX_DS_BYTES = (size_t)2 << 30;
 BwdPlan plan_backward(const AttnPlan& p) {
   const sh_attention& a = p.a;
@@ -235,7 +245,7 @@ BwdPlan plan_backward(const AttnPlan& p) {
     }
     b.ds_ld = ceil_div(rows, PACKED_BM) * PACKED_BM;
     const size_t ds = (size_t)a.nkv_heads * a.total_k * b.ds_ld * 2;
-    if (ds > 0 && ds <= MAX_DS_BYTES) {
+    if (a.d_head > 64 && ds > 0 && ds <= MAX_DS_BYTES) {
       b.ds = off;
       off += align_up(ds);
     }

@@ -54,7 +54,7 @@ struct PackedAttnBwd {
   const void* dO;
   const float* delta;                  // [H][total_q]
   void *dQ, *dK, *dV;
-  // bf16, head widths up to 128: score gradients dS^T [kv head][key][row of the sequence], rows of ds_ld, or NULL: computed again for dQ
+  // bf16, head widths of 65 .. 128: score gradients dS^T [kv head][key][row of the sequence], rows of ds_ld, or NULL: computed again for dQ
   void* dS;
   long ds_ld;
   // rows of a dK / dV work-group (a multiple of PACKED_QT): key tiles that see more leave fp32 parts, [part][slot * Hk + kv head][dV, dK] of

@@ -201,6 +201,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
   constexpr int QT = PACKED_QT, KB = PACKED_KB, LD = DH == 128 ? 128 : DH + 16, NST = 3, NKD = DH / 16, NDB = DH / 32, CPR = DH / 8, TOTAL = QT * CPR, NCH = (TOTAL + 255) / 256;
   constexpr int SK = DH <= 96 ? 2 : 1, SR = QT / 32 / SK;   // key blocks and row blocks of a score wave
   constexpr int STAGE = 2 * QT * LD;
+  constexpr bool KEEP = DH > 64;   // (narrower heads keep no score gradients: plan_backward)
   __shared__ __attribute__((aligned(16))) unsigned short tiles[NST * STAGE];
   __shared__ __attribute__((aligned(16))) uint4 hand[2][4][8][64];   // [buffer][key block][P, dS of 16 rows in turn][lane]
   static_assert(sizeof tiles + sizeof hand <= 160 * 1024, "fits a CU");
@@ -329,7 +330,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
             hd[(2 * h + 1) * 64] = ud.q;
             // elements 0..3 / 4..7: rows r0 + 16 h + 4 g + {0..3} / + 8 + {0..3} of this lane's key; the lane halves trade, so that each has 8 rows side by side
             const auto lo = __builtin_amdgcn_permlane32_swap(ud.q.x, ud.q.z, false, false), hi = __builtin_amdgcn_permlane32_swap(ud.q.y, ud.q.w, false, false);
-            if (b.dS && key < s.lk) *(uint4*)(dsrow[k] + r0 + 16 * h) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+            if (KEEP && b.dS && key < s.lk) *(uint4*)(dsrow[k] + r0 + 16 * h) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
           }
         }
       }
@@ -644,10 +645,12 @@ static void launch_bwd_al(const PackedAttnBwd& b, hipStream_t s) {
   } else if constexpr (sizeof(T) == 2 && DH <= 128) {
     packed_dkv_ws_kernel<DH, AL><<<dim3((unsigned)((b.klevels ? (long)b.klevels * a.nseq * a.Hk : kslots) * b.rparts)), 512, 0, s>>>(b);
     if (b.rparts > 1) packed_dkv_join_kernel<DH, AL><<<gk, 512, 0, s>>>(b);
-    if (b.dS && a.total_q > 0) {
-      prof_mark(s, "attention.dq");
-      packed_dq_ds_kernel<DH, AL><<<gq, 256, 0, s>>>(b);
-      return;
+    if constexpr (DH > 64) {
+      if (b.dS && a.total_q > 0) {
+        prof_mark(s, "attention.dq");
+        packed_dq_ds_kernel<DH, AL><<<gq, 256, 0, s>>>(b);
+        return;
+      }
     }
   } else {
     packed_dkv_kernel<T, DH, AL, 0><<<gk, 256, 0, s>>>(b);

@@ -109,3 +109,19 @@ def test_gradients_when_every_key_is_visible_and_none_is_queried():
         for causal in (0, 1):
             for dtype in ("f32", "bf16"):
                 Packed(4, 2, 64, dtype, nq, nk, causal=causal, seed=45).check(backward=True, max_q=max(max(nq), 1), max_k=max(max(nk), 1))
+
+
+@pytest.mark.parametrize("H,Hk,d", [(4, 1, 128), (4, 1, 76)])
+def test_more_score_gradients_than_are_kept(H, Hk, d):
+    """Wide heads whose score gradients would take more than 2 GiB: dQ works the scores out again.  Narrow heads keep none at any size."""
+    p = Packed(H, Hk, d, "bf16", [300, 1, 33], seed=46)
+    few = binding.make_attention(p.q, p.k, p.v, p.q, 3, 300, 300)
+    assert binding.switchhead_attention_workspace_bytes(few, True) >= p.k.shape[0] * 1200 * 2
+    p.check(backward=True)
+    p.k, p.v = (torch.cat((t, torch.full((1 << 20, Hk, d), 3.0, dtype=t.dtype))) for t in (p.k, p.v))   # rows of no sequence
+    many = binding.make_attention(p.q, p.k, p.v, p.q, 3, 300, 300)
+    assert binding.switchhead_attention_workspace_bytes(many, True) < p.k.shape[0] * 1200 * 2
+    p.check(backward=True)
+    n = Packed(4, 1, 64, "bf16", [1200], seed=47)
+    plan = binding.make_attention(n.q, n.k, n.v, n.q, 1, 1200, 1200)
+    assert binding.switchhead_attention_workspace_bytes(plan, True) < 1200 * 4800 * 2
