@@ -6,7 +6,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 from paper_2312_07987_amd import binding
-from test_gpu_attention_ops import Packed
+from test_gpu_attention_ops import Packed, close, norm_oracle
 
 pytestmark = pytest.mark.gpu
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
@@ -125,3 +125,62 @@ def test_more_score_gradients_than_are_kept(H, Hk, d):
     n = Packed(4, 1, 64, "bf16", [1200], seed=47)
     plan = binding.make_attention(n.q, n.k, n.v, n.q, 1, 1200, 1200)
     assert binding.switchhead_attention_workspace_bytes(plan, True) < 1200 * 4800 * 2
+
+
+def laid(t, layout):
+    """t's values on the GPU, head by head (rows of all tokens of a head behind each other), or beginning one element behind an aligned address."""
+    if layout == "by head":
+        return t.transpose(0, 1).contiguous().cuda().transpose(0, 1)
+    flat = torch.empty(t.numel() + 1, dtype=t.dtype, device="cuda")
+    out = flat[1:].view(t.shape)
+    out.copy_(t)
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["by head", "odd address"])
+@pytest.mark.parametrize("H,Hk,d", [(4, 2, 64), (2, 2, 128), (2, 1, 76)])
+def test_other_layouts(H, Hk, d, layout, dtype):
+    p = Packed(H, Hk, d, dtype, [70, 1, 130], seed=48)
+    ref = p.reference(backward=True)
+    bounds = ref.pop("bounds")
+    q, k, v, dO = (laid(t, layout) for t in (p.q, p.k, p.v, p.dO))
+    O, dq, dk, dv = (laid(torch.full(t.shape, 777.0, dtype=t.dtype), layout) for t in (p.q, p.q, p.k, p.v))
+    lse, off = torch.empty(H, p.q.shape[0], device="cuda"), i32(p.qoff)
+    plan = binding.make_attention(q, k, v, O, 3, 130, 130)
+    ws = torch.full((max(binding.switchhead_attention_workspace_bytes(plan, b) for b in (False, True)),), 255, dtype=torch.uint8, device="cuda")
+    binding.switchhead_attention_forward(plan, q, k, v, off, off, O, lse, ws)
+    binding.switchhead_attention_backward(plan, q, k, v, O, dO, lse, off, off, dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    close("O", O, ref["O"], dtype)
+    close("dV", dv, ref["dV"], dtype)
+    for n, t in (("dQ", dq), ("dK", dk)):
+        assert float(((t.double().cpu() - ref[n]).abs() - bounds[n]).max()) <= 0, n
+    one = Packed(H, Hk, d, dtype, [1, 1, 1], [70, 1, 300], seed=49)   # single tokens
+    q, k, v = (laid(t, layout) for t in (one.q, one.k, one.v))
+    O = laid(torch.zeros_like(one.q), layout)
+    plan = binding.make_attention(q, k, v, O, 3, 1, 300)
+    ws = torch.empty(binding.switchhead_attention_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+    binding.switchhead_attention_forward(plan, q, k, v, i32(one.qoff), i32(one.koff), O, None, ws)
+    torch.cuda.synchronize()
+    close("token", O, one.reference()["O"], dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["by head", "odd address"])
+@pytest.mark.parametrize("tokens", [1, 37])
+def test_norms_of_other_layouts_in_place(tokens, layout, dtype):
+    """Forward into the input and gradients into the upstream gradient, which lies as they do."""
+    g = torch.Generator().manual_seed(50)
+    x, dy = (torch.randn(tokens, 4, 64, generator=g).to(DT[dtype]) for _ in range(2))
+    dx, dw = laid(dy, layout), torch.empty(64, device="cuda")
+    kept, y = laid(x, layout), laid(x, layout)
+    plan = binding.make_qk_norm(kept, None, y, None, 32)
+    binding.switchhead_qk_norm_rope_forward(plan, y, None, None, None, None, y, None)
+    ws = torch.empty(binding.switchhead_qk_norm_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+    binding.switchhead_qk_norm_rope_backward(plan, kept, None, None, None, None, dx, None, dx, None, dw, None, ws)
+    torch.cuda.synchronize()
+    ry, rdx, rdw = norm_oracle(x, None, torch.arange(tokens), 32, 1e-6, 10000.0, dy)
+    close("y", y, ry, dtype)
+    close("dx", dx, rdx, dtype)
+    close("dw", dw, rdw, "f32", scale=max(float(rdw.norm()), math.sqrt(tokens * 4 * 64)))

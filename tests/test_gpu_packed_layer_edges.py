@@ -7,7 +7,7 @@ from oracle import switchhead_oracle as orc
 from paper_2312_07987_amd import binding
 from paper_2312_07987_amd.inputs import make_inputs
 from paper_2312_07987_amd.runner import DeviceLayer
-from test_gpu_packed_layer import BF, F32, NAMES, close, reference
+from test_gpu_packed_layer import BAR, BF, F32, NAMES, close, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -15,7 +15,7 @@ pytestmark = pytest.mark.gpu
 class PackedCall:
     """A layer, its packing and its workspace on the GPU; forward() and backward() are the calls."""
 
-    def __init__(self, cfg, offsets, rows, norm, eps, host=None, seed=3, dense=False):
+    def __init__(self, cfg, offsets, rows, norm, eps, host=None, seed=3, dense=False, max_len=None):
         self.cfg = dict(cfg, B=1, T=rows)
         self.host = make_inputs(self.cfg, seed=seed) if host is None else host
         self.layer = DeviceLayer(self.cfg, self.host, dense=dense)
@@ -23,7 +23,7 @@ class PackedCall:
         g = torch.Generator().manual_seed(5)
         self.w = [(1 + 0.2 * torch.randn(d, generator=g)).to(self.layer.tdtype) for _ in range(2)] if norm else None
         self.offsets = torch.tensor(offsets, dtype=torch.int32, device="cuda")
-        self.packing = binding.make_packing(self.offsets, rows, *([v.cuda() for v in self.w] if norm else (None, None)), norm_eps=eps)
+        self.packing = binding.make_packing(self.offsets, rows if max_len is None else max_len, *([v.cuda() for v in self.w] if norm else (None, None)), norm_eps=eps)
         self.ws = torch.full((binding.switchhead_packed_workspace_bytes(self.layer.shape, self.packing),), 255, dtype=torch.uint8, device="cuda")
         self.dn = [torch.empty(d, device="cuda") if norm else None for _ in range(2)]
 
@@ -131,3 +131,49 @@ def test_captured_and_replayed_with_other_lengths(base):
         step()
         for n, t in p.results().items():
             close(n, again[n], t.double().cpu(), "f32")   # (weight gradients may be added with fp32 atomics: not to the last bit)
+
+
+def leftover(host, cfg, f, at):
+    """What a sequence of one token may leave in dW_Q and dW_K, whose exact part is 0: its probability is 1, O = V to the bit, and dS = <dO, V> - <dO, O> is the
+    difference of two sums of the same d products in two orders, each within d 2^-23 |dO| |V| (2^-23: sums that cut instead of rounding).
+    dO is the gated sum of W_O dy, gates at most 1; an element of dW_Q is x s dS K, of dW_K x s dS Q."""
+    d, most = cfg["d_head"], 0.0
+    x, dy = host["x"][0, at.start].astype(np.float64), host["dy"][0, at.start].astype(np.float64)
+    for h in range(cfg["nheads"]):
+        dO = sum(np.linalg.norm(w.astype(np.float64) @ dy) for w in host["W_O"][h])
+        Q, K, V = (np.linalg.norm(np.asarray(f[n], dtype=np.float64).reshape(-1, cfg["nheads"], d)[0, h]) for n in ("Q", "K", "V"))
+        most = max(most, np.abs(x).max() * d ** -0.5 * 2 * d * 2.0 ** -23 * dO * V * max(Q, K))
+    return most
+
+
+@pytest.mark.parametrize("base", [F32, BF], ids=["f32", "bf16"])
+@pytest.mark.parametrize("offsets,max_len", [([0, 40, 60], 25), ([0, 0, 1, 1, 1], 60), ([59, 60, 60], 1), ([0, 60], 1000)])
+def test_bounds_on_the_lengths_and_empty_sequences(base, offsets, max_len):
+    """Rows past max_len are rows of no sequence; empty sequences and single rows."""
+    cfg, rows = dict(base, rope=1), 60
+    host = make_inputs(dict(cfg, B=1, T=rows), seed=12)
+    p = PackedCall(cfg, offsets, rows, False, 0.0, host, max_len=max_len)
+    p.forward()
+    p.backward()
+    got = p.results()
+    want = dict(y=np.zeros((1, rows, cfg["d_model"])), dx=np.zeros((1, rows, cfg["d_model"])), **{"d" + n: np.zeros(host[n].shape) for n in NAMES})
+    none, rest = torch.ones(rows, dtype=torch.bool), 0.0
+    for a, b in zip(offsets[:-1], offsets[1:]):
+        at = slice(a, min(b, a + max_len))
+        if at.start == at.stop:
+            continue
+        none[at] = False
+        f = orc.forward(host["x"][:, at], *[host[m] for m in NAMES], None, None, k=cfg["k"], causal=True, rope=True, T_q=None)
+        g = orc.backward(host["x"][:, at], *[host[m] for m in NAMES], f, host["dy"][:, at])
+        want["y"][:, at], want["dx"][:, at] = f["y"], g["dx"]
+        for n in NAMES:
+            want["d" + n] += g["d" + n]
+        if at.stop - at.start == 1:
+            rest += leftover(host, cfg, f, at)
+    for n in ("y", "dx"):
+        assert torch.all(got[n][0][none.cuda()] == 0), n
+    for n, w in want.items():
+        slack = rest if n in ("dW_Q", "dW_K") else 0.0
+        err, most = float((got[n].double().cpu() - torch.from_numpy(w)).abs().max()), float(np.abs(w).max())
+        print(n, err, most, slack, flush=True)
+        assert err <= BAR[cfg["dtype"]] * most + slack, n
