@@ -269,14 +269,15 @@ sh_status switchhead_get_intermediates(const sh_shape* shape,
  * q_lengths (k_lengths) only the first q_lengths[i] (k_lengths[i]) of them, as in a padded batch or a cache with a place of one
  * length per sequence.  All four are int32 arrays on the device (offsets nseq + 1, lengths nseq; lengths may be NULL).  Offsets
  * must not fall.  They are not checked on the host; whatever they hold, no row outside the tensors is touched.
- * Rows that belong to no sequence are neither read nor written.
+ * Rows that belong to no sequence have no influence and are not written (they may be read: the tensors' memory must be there).
  *
  *   O_i = sum_u p_iu V_u,   p_iu = exp(scale <Q_i, K_u> - lse_i),   lse_i = log sum_u exp(scale <Q_i, K_u>)
  *
  * over the keys u that query i of its sequence sees: all rows of the prefix, and of its n_k own keys all, or with `causal` those
  * with u <= (n_k - n_q) + i (the last query sees every key).  A query that sees nothing has O = 0, lse = -infinity and gives
  * no gradient.  What lies in keys and values behind a sequence's length has no influence, NaN included; a NaN or an infinity in
- * a value that only `causal` hides may reach a query all the same (0 x NaN in a product), and in a key its gradients.
+ * a value that only `causal` hides may reach a query all the same (0 x NaN in a product), and in a key, a query or a row of dO the gradients
+ * of the rows that it is hidden from.
  */
 typedef struct {
   int32_t nseq;
@@ -358,7 +359,7 @@ typedef struct {
   const int32_t* offsets;
   const void *q_norm, *k_norm;  /* [d_head] in storage type: weights of the norms of queries and keys (x w /
                                    sqrt(mean(x^2) + norm_eps), before the rotation); both NULL: no norms             */
-  float norm_eps;
+  float norm_eps;               /* >= 0; with 0 a query or key of a sequence that is all zeros has no norm (NaN)      */
 } sh_packing;
 
 /* Bytes of workspace of the two calls below; 0 if shape or packing are invalid.  Host-only (offsets may be NULL).

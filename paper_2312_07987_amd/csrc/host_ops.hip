@@ -227,9 +227,10 @@ BwdPlan plan_backward(const AttnPlan& p) {
   b.rparts = 1;
   if (a.dtype == SH_BF16 && a.d_head <= 128 && rows > 0) {
     // Rows of a dK / dV work-group: what a CU would get if every key tile were seen by the longest rows there are.  Parts cost their writing and a second
-    // kernel, so they are for launches with a few tiles far longer than the rest.  A step with 100 / 50 / 35 / 20 per cent of this, us: 16384 tokens
-    // of 4 heads of 128, longest 4096, 304 (297 without parts) / 334 / 336 / 359; 6600 tokens of 20 heads over 4, longest 4096, 597 / 629 / 623 / 637 (743 without
-    // parts); 4096 tokens of 8 heads over 2 311 / 322 / 327 / 350 (639).  At least 512, where a work-group is about as long as its start and the extra parts.
+    // kernel, so they are for launches with a few tiles far longer than the rest.  Forward and backward with 100 / 50 / 35 / 20 per cent of this and without parts, us: 6600
+    // tokens of 20 heads of 80 over 4, longest 4096, 598 / 630 / 622 / 639 and 745; 4096 tokens of 8 heads of 128 over 2 308 / 321 / 326 / 345 and 646; 16384 tokens of 4
+    // heads of 128, longest 4096 (no parts at 100 and 50 per cent, whose ranges hold all rows) 305 / 306 / 328 / 340 and 307.  At least 512, where a work-group is about as
+    // long as its start and the extra parts.
     const long tiles = ceil_div(a.total_k, PACKED_KB) * a.nkv_heads;
     long chunk = tiles * rows / 256;
     chunk = ceil_div(chunk < 512 ? 512 : chunk, PACKED_QT) * PACKED_QT;
@@ -384,7 +385,8 @@ sh_status switchhead_attention_forward(const sh_attention* d, const void* Q, con
     return fail(SH_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if ((r = check_workspace(workspace, workspace_bytes, p.total)) != SH_OK) return r;
   if (s.nseq == 0 || s.total_q == 0 || s.max_q == 0) return SH_OK;
-  if (any_same({O}, {K, V, K_prefix, V_prefix})) return fail(SH_ERR_INVALID_ARG, "O lies over keys or values");
+  const void *const k = s.total_k ? K : nullptr, *const v = s.total_k ? V : nullptr, *const kp = s.prefix ? K_prefix : nullptr, *const vp = s.prefix ? V_prefix : nullptr;
+  if (any_same({O}, {k, v, kp, vp})) return fail(SH_ERR_INVALID_ARG, "O lies over keys or values");
   const hipStream_t st = (hipStream_t)hip_stream;
   const int bf16 = s.dtype == SH_BF16;
   const int align = alignment({Q, K, V, O, K_prefix, V_prefix}, {s.q_row, s.q_head, s.k_row, s.k_head, s.v_row, s.v_head, s.o_row, s.o_head, s.kp_row, s.kp_head, s.vp_row, s.vp_head},
