@@ -389,7 +389,7 @@ void launch_packed_prefix(const PackedAttn& f, const PackedAttn& o, bool few, in
 void launch_packed_join(const PackedAttn& a, int bf16, hipStream_t s);
 void launch_packed_bwd(const PackedAttnBwd& a, int bf16, int align, float* delta, hipStream_t s);
 
-enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128, PACKED_QT = 64 };
+enum { PACKED_BM = 128, PACKED_BM2 = 256, PACKED_FEW = 16, PACKED_KB = 128, PACKED_QT = 64, PACKED_EXACT = 32 };
 // head width that a work-group's tiles are laid out for
 static inline int packed_width(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : dh <= 96 ? 96 : dh <= 128 ? 128 : 256; }
 // lanes that share a row of the backward pass' <dO, O>: 16 bytes each

@@ -20,10 +20,15 @@ __device__ __forceinline__ bool row_tile(const PackedAttn& a, int id, int& row0,
   return true;
 }
 
-// delta[head][token] = <dO, O>, from the rows as they are stored: LR lanes hold a row in 16-byte pieces.  O's rounding to bf16 is an error of P delta
-// that a form with O in 32 bits has not; the exact delta would be a pass over the keys of its own (sum P dP, 4 d of 10 d operations again).  Relative 2-norm error of dQ
-// and dK with the results and dS rounded alone 2.4e-3, with this 2.5e-3 (1500 tokens, heads of 128) to 2.7e-3 (20 to 256 tokens, heads of 76); dV has none of it.
-// (Rows of no sequence are summed too; nothing reads those sums.)
+// delta[head][token] = <dO, O>, from the rows as they are stored: LR lanes hold a row in 16-byte pieces.  (Rows of no sequence are summed too; nothing reads those sums.)
+//
+// O's rounding to bf16 is an error of P delta in dS = P (dP - delta) that a form with O in 32 bits has not.  It counts where a row sees few keys: the more keys a row averages
+// over, the smaller its O, and the smaller its P beside dP.  So for bf16 rows that see up to PACKED_EXACT (32) keys the kernels below take delta = sum P dP instead, which
+// needs no O: all those keys are one block of their products.  Relative 2-norm error of dQ and dK with the results' and dS's roundings alone / with delta exact up to
+// 32, 16 and no keys (float64 arithmetic, roundings put in one at a time): 96 sequences of 20 to 256 tokens, heads of 76, 2.35e-3 / 2.37, 2.40, 2.62; 1500 tokens, heads of
+// 128, 2.36e-3 / 2.38, 2.39, 2.57.  It costs 1.4 to 2.8 us of a step over 96 such short sequences (44 and 52 us), 1 per cent of one over long ones; in the
+// kernels below the block with such rows is a branch of its own, element after element, so that the others keep their registers.  (In a launch of its own, or tile by tile with <dO, O>:
+// 4 to 5 us.)  Exact for all rows would be the forward pass' operations once more.
 template <typename T, int LR, int AL>
 __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn a, const void* dO_, float* delta) {
   typedef typename Elem<T>::raw raw;
@@ -48,6 +53,21 @@ __global__ __launch_bounds__(256) void packed_delta_kernel(PackedAttn a, const v
 #pragma unroll
   for (int k = 1; k < LR; k <<= 1) x += __shfl_xor(x, k, 64);
   if (d == 0) delta[(long)head * a.total_q + tok] = x;
+}
+
+// The first rows of a sequence, which see up to PACKED_EXACT keys: how many they are
+__device__ __forceinline__ int exact_rows(const PackedAttn& a, const SeqGeom& s) {
+  if (a.causal) return min(max(PACKED_EXACT - (s.lk - s.lq), 0), s.lq) * a.G;
+  return s.lk <= PACKED_EXACT ? s.lq * a.G : 0;
+}
+// the sum of a lane half's 32 values, in all of its lanes
+__device__ __forceinline__ float half_sum(float x) {
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0xB1, 0xF, 0xF, true));    // lane ^ 1
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x4E, 0xF, 0xF, true));    // ^ 2
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x141, 0xF, 0xF, true));   // the other four of eight
+  x += __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), 0x140, 0xF, 0xF, true));   // the other eight of sixteen
+  const auto v = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(v[0]) + __uint_as_float(v[1]);
 }
 
 // dK and dV of 128 keys of one (sequence, kv head): 4 waves x 32 keys, whose K and V rows are registers; tiles of 32 rows of Q and dO go
@@ -83,6 +103,7 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
     if constexpr (DV) accV[d] = zero16();
   }
   const float sc = a.scale * 1.44269504088896340736f;
+  const int exact = exact_rows(a, s);
   // the first row that sees one of the keys
   const int rbeg = a.causal ? max(k0 - off, 0) * a.G / QT * QT : 0;
 
@@ -131,19 +152,30 @@ __global__ __launch_bounds__(256, 1) void packed_dkv_kernel(PackedAttnBwd b) {
       if constexpr (DK) dP = mma32(row_frag(&Gs[r * LD + kk * 16 + 8 * g]), vf[kk], dP);
     }
     float p[16], ds[16];
+    const bool few = r0 < exact && k0 + wave == 0;   // uniform: the block has all keys of some of its rows
     const bool masked = r0 + QT > rows || k0 + wave * 32 + 32 > s.lk || (a.causal && k0 + wave * 32 + 31 > div_by(r0, a.g_inv) + off);
+    auto visible = [&](int rr) { return r0 + rr < rows && key < s.lk && (!a.causal || key <= div_by(r0 + rr, a.g_inv) + off); };
+    if (sizeof(T) == 2 && DK && few) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int rr = 8 * (i >> 2) + 4 * g + (i & 3);
-      float arg = fmaf(S[i], sc, -lse_s[rr]);
-      if (masked) {
-        const bool vis = r0 + rr < rows && key < s.lk && (!a.causal || key <= div_by(r0 + rr, a.g_inv) + off);
-        arg = vis ? arg : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const int rr = 8 * (i >> 2) + 4 * g + (i & 3);
+        p[i] = visible(rr) ? __builtin_amdgcn_exp2f(fmaf(S[i], sc, -lse_s[rr])) : 0.f;
+        const float t = half_sum(visible(rr) ? p[i] * dP[i] : 0.f);
+        ds[i] = visible(rr) ? p[i] * (dP[i] - (r0 + rr < exact ? t : del_s[rr])) : 0.f;
+        asm volatile("" : "+v"(ds[i]));
+        __builtin_amdgcn_sched_barrier(0);   // (one after the other: the registers are full)
       }
-      p[i] = __builtin_amdgcn_exp2f(arg);
-      if constexpr (DK) {
-        ds[i] = p[i] * (dP[i] - del_s[rr]);
-        if (masked && arg == -INFINITY) ds[i] = 0.f;   // (what a hidden row or key holds stays out)
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int rr = 8 * (i >> 2) + 4 * g + (i & 3);
+        float arg = fmaf(S[i], sc, -lse_s[rr]);
+        if (masked) arg = visible(rr) ? arg : -INFINITY;
+        p[i] = __builtin_amdgcn_exp2f(arg);
+        if constexpr (DK) {
+          ds[i] = p[i] * (dP[i] - del_s[rr]);
+          if (masked && arg == -INFINITY) ds[i] = 0.f;   // (what a hidden row or key holds stays out)
+        }
       }
     }
 #pragma unroll
@@ -246,6 +278,7 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
       dsrow[k] = (raw16*)b.dS + (b.dS ? ((long)hk * a.total_k + kc) * b.ds_ld + 8 * g : 0);
     }
     const float sc = a.scale * 1.44269504088896340736f;
+    const int exact = exact_rows(a, s);
     // the statistics of the next tile's rows (lane half 0: lse, 1: delta; rows past the end repeat the last one)
     float st[SR];
     auto statistics = [&](int r0) {
@@ -303,10 +336,23 @@ __global__ __launch_bounds__(512, 1) void packed_dkv_ws_kernel(PackedAttnBwd b) 
           const int wk = k0 + (kb0 + k) * 32, key = wk + r;
           const f32x16 S = S_[blk][k], dP = dP_[blk][k];
           float p[16], ds[16];
+          if (wk == 0 && r0 < exact) {   // uniform: the block has all keys of some of its rows
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L_[blk][i / 4][i % 4]));
-            ds[i] = p[i] * (dP[i] - D_[blk][i / 4][i % 4]);
+            for (int i = 0; i < 16; ++i) {
+              const int rr = r0 + 8 * (i >> 2) + 4 * g + (i & 3);
+              const bool vis = rr < rend && key < s.lk && (!a.causal || key <= div_by(rr, a.g_inv) + off);
+              p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L_[blk][i / 4][i % 4]));
+              const float t = half_sum(vis ? p[i] * dP[i] : 0.f);
+              ds[i] = p[i] * (dP[i] - (rr < exact ? t : D_[blk][i / 4][i % 4]));
+              asm volatile("" : "+v"(ds[i]));
+              __builtin_amdgcn_sched_barrier(0);   // (one after the other: the registers are full)
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              p[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -L_[blk][i / 4][i % 4]));
+              ds[i] = p[i] * (dP[i] - D_[blk][i / 4][i % 4]);
+            }
           }
           // wave-uniform: most blocks lie wholly inside the visible region
           if (r0 + 32 > rend || wk + 32 > s.lk || (a.causal && wk + 31 > div_by(r0, a.g_inv) + off)) {
@@ -574,13 +620,13 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
   const int wq_first = div_by(min(row0 + wave * 32, rows - 1), a.g_inv) + off;
   const int wq_last = div_by(min(row0 + wave * 32 + 31, rows - 1), a.g_inv) + off;
   const int last_tok = div_by(min(row0 + BM, rows) - 1, a.g_inv);
-  const int kend = max(0, a.causal ? min(s.lk, last_tok + off + 1) : s.lk);
+  const int kend = max(0, a.causal ? min(s.lk, last_tok + off + 1) : s.lk), exact = exact_rows(a, s);
 
   frag_t<T> qf[NKD], gf[NKD];
   const raw* Q = (const raw*)a.Q + (long)(s.qbeg + tok) * a.q_row + (long)head * a.q_head;
   const raw* G = (const raw*)b.dO + (long)(s.qbeg + tok) * a.o_row + (long)head * a.o_head;
   const float lse2 = a.lse[(long)head * a.total_q + s.qbeg + tok] * 1.44269504088896340736f;
-  const float del = b.delta[(long)head * a.total_q + s.qbeg + tok];
+  float del = b.delta[(long)head * a.total_q + s.qbeg + tok];
   f32x16 acc[NDB];
 #pragma unroll
   for (int d = 0; d < NDB; ++d) acc[d] = zero16();
@@ -618,6 +664,16 @@ __global__ __launch_bounds__(256, DH* sizeof(T) > 256 ? 1 : 2) void packed_dq_ke
       }
       float ds[16];
       const int lim = (a.causal ? min(kend - 1, qpos) : kend - 1) - (k0 + kb * 32 + 4 * g);
+      if (sizeof(T) == 2 && k0 + kb == 0 && row0 + wave * 32 < exact) {   // uniform; a row is a lane of either half
+        float t = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          if (8 * (i >> 2) + (i & 3) <= lim) t = fmaf(__builtin_amdgcn_exp2f(fmaf(S[i], sc, -lse2)), dP[i], t);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        t += __shfl_xor(t, 32, 64);
+        del = row < exact ? t : del;
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         ds[i] = __builtin_amdgcn_exp2f(fmaf(S[i], sc, -lse2)) * (dP[i] - del);
